@@ -300,10 +300,144 @@ typedef enum {
    * small bf16 batches) never give up: a workgroup that has waited for the others for this
    * long, or for 0.1 ms and a time that grows with the work if that is less, does what is
    * missing itself, with the same results. */
-  FINCH_OPT_LAYER_WAIT_TICKS = 5
+  FINCH_OPT_LAYER_WAIT_TICKS = 5,
+  /* rows that share a power of two in an 8-bit cache (finch_quantize, finch_attend): 16, 32, 64
+   * (default) or 128 */
+  FINCH_OPT_SCALE_BLOCK = 6
 } finch_option;
 typedef enum { FINCH_PATH_AUTO = 0, FINCH_PATH_SEPARATE = 1, FINCH_PATH_OWNER = 3 } finch_path;
 finch_status finch_set_option(finch_ctx* ctx, int32_t option, int64_t value);
+
+/* ------------------------------------------------------------------------------------
+ * Around the compression, in the layer it serves: the rows of a layer's projections become
+ * the rows that scoring and attention read (finch_rotate), the attention itself over
+ * [cache ; chunk] (finch_attend: prefill of a chunk, and the generation stage from the
+ * compressed cache), and that cache in 8 bits (finch_quantize).  Same conventions as above:
+ * one context per thread and stream, descriptors on the host and on the device, no
+ * allocation, no synchronisation, argument errors before anything is launched, results
+ * bit-identical run to run.  Strides are in elements of the rows' type; every row and
+ * head has to start at a multiple of 16 bytes, channels of a head lie one after the other.
+ * These calls run on the context's device, whatever device is current; the three may be
+ * captured into a HIP graph.  finch_profile does not record them.
+ */
+
+/* Rows of one request out of its projections: token t, query head h of the kv_heads * G ones
+ * is at q + t*q_row + h*q_head, and goes to q_out + t*q_out_row + h*q_out_head; keys and
+ * values the same for kv_heads heads, except that token t goes to row slot[t] of k_out and
+ * v_out where `slot` is given (appending to a cache, whose pages may lie in any order).  A
+ * slot outside 0 .. slots-1 drops the token's key and value (padding); slots of one call
+ * must be distinct.  q, k or v NULL: that part is left out.  An output may be its own input
+ * (same pointer and strides, no slots); other overlaps are the caller's to avoid. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* q_out;
+  void* k_out;
+  void* v_out;
+  const int32_t* pos;  /* device, [n] positions (any int32); NULL: pos0 + t   */
+  const int32_t* slot; /* device, [n] rows of k_out and v_out; NULL: row t    */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  int64_t q_out_row, q_out_head, k_out_row, k_out_head, v_out_row, v_out_head;
+  int32_t n;           /* tokens, >= 0                                        */
+  int32_t kv_heads;    /* >= 1                                                */
+  int32_t pos0;
+  int32_t slots;       /* rows of k_out and v_out; read only with `slot`      */
+} finch_rows;
+
+/* What happens to queries and keys on the way (values are copied bit for bit):
+ *   y = x * w / sqrt(mean(x^2) + eps)      over the head's channels, if a weight is given
+ *   (a, b) -> gain * (a cos t - b sin t, b cos t + a sin t),  t = pos * freq[u]
+ * for channel pairs u < dims/2 of the first `dims` channels: (u, u + dims/2) for
+ * FINCH_ROPE_HALF, (2u, 2u+1) for FINCH_ROPE_INTERLEAVED; the other channels stay.  In fp32
+ * (angles reduced in fp64), rounded once, to nearest even. */
+typedef struct {
+  int32_t pairing;     /* finch_rope_pairing; FINCH_ROPE_OFF: no rotation     */
+  int32_t dims;        /* rotated channels: a multiple of 16, 16 .. head_dim  */
+  const double* freq;  /* device, [dims/2] radians per position               */
+  const void* q_norm;  /* device, [head_dim] weights in the context's dtype, 16-byte aligned; NULL: no norm */
+  const void* k_norm;
+  float eps;           /* >= 0                                                */
+  float gain;
+} finch_rotary;
+
+finch_status finch_rotate(finch_ctx* ctx, const finch_rotary* how, const finch_rows* host_desc,
+                          const finch_rows* dev_desc, int32_t n_requests, void* stream);
+
+/* Host-only: the table freq[u] = base^(-2u/dims), u < dims/2, and what long contexts make of it.
+ *   LINEAR  freq / factor (positions interpolated)
+ *   BANDED  by the number of turns T = context * freq / 2 pi over the context a model was trained
+ *           on: freq / factor where T <= low, freq where T >= high, a linear mix in T between
+ *   RAMP    the mix is linear in the channel pair, from the pair that turns `high` times (rounded
+ *           down, not below 0) to the one that turns `low` times (rounded up, at most dims - 1);
+ *           its gain is 0.1 ln(factor) + 1
+ * Writes dims/2 values and the gain (1 otherwise); freq_len is the capacity of freq. */
+typedef enum { FINCH_SCALING_NONE = 0, FINCH_SCALING_LINEAR = 1, FINCH_SCALING_BANDED = 2, FINCH_SCALING_RAMP = 3 } finch_scaling;
+typedef struct {
+  int32_t kind;     /* finch_scaling                                          */
+  int32_t reserved; /* must be 0                                              */
+  double factor;    /* >= 1                                                   */
+  double low, high; /* BANDED, RAMP: turns, 0 < low < high                    */
+  double context;   /* BANDED, RAMP: tokens, > 0                              */
+} finch_rope_scaling;
+finch_status finch_rope_frequencies(int32_t dims, double base, const finch_rope_scaling* scaling, double* freq,
+                                    int32_t freq_len, float* gain);
+
+/* The cache in 8 bits.  Rows are cut into blocks of FINCH_OPT_SCALE_BLOCK; a block of one head's
+ * keys (and one of its values) has one power of two 2^e, the smallest with max|x| <= 448 * 2^e
+ * and e >= -100 (e = 0 for a block of zeros), held as the byte e + 127, and its rows hold the
+ * e4m3 numbers nearest to x / 2^e (ties to even): a value loses at most 2^-4 of itself, or
+ * 2^(e-10) where it is below 2^(e-6).  No value overflows, and the products by powers of
+ * two are exact, so the bytes do not depend on how they are computed. */
+typedef struct {
+  const void* k;    /* [n] rows in the context's dtype, in_row elements apart */
+  const void* v;
+  uint8_t* k_out;   /* [n] rows of head_dim bytes, out_row bytes apart        */
+  uint8_t* v_out;
+  uint8_t* k_scale; /* [ceil(n / block)]                                      */
+  uint8_t* v_scale;
+  int64_t in_row, out_row;
+  int32_t n;        /* >= 0                                                   */
+  int32_t reserved; /* must be 0                                              */
+} finch_quantization;
+finch_status finch_quantize(finch_ctx* ctx, const finch_quantization* host_desc, const finch_quantization* dev_desc,
+                            int32_t n_problems, void* stream);
+
+/* Attention of the rows of a KV head's G query heads (Background, attention equation) over its
+ * candidates [cache ; chunk], c + m of them:
+ *   out[i][g] = sum_j softmax_j( q[i][g] . k_j / sqrt(d_k) ) v_j
+ * over the candidates row i sees: all of them, or with `causal` the c + m - n_que + i + 1 first
+ * ones (the rows are the last n_que tokens of the chunk; fewer than one: none).  A row that sees
+ * nothing gives zeros, and -inf in lse.  n_que = 1 is a generated token, whose own key is the
+ * last row of the chunk.  Weights are rounded to bf16 before they meet values of bf16.
+ * With k_scale and v_scale (both or neither, bf16 contexts only) the cache rows are those of
+ * finch_quantize, and cache_row counts bytes.  With m_live the chunk has min(m, max(0,
+ * *m_live)) rows when the kernel runs, so that a captured step can go on being replayed
+ * while its chunk grows.  q and out may be views of [token][head][channel] arrays of a packed
+ * batch.  `out` must overlap neither q nor candidates, nor lie over itself: one of its two strides
+ * must step over all of the other's. */
+typedef struct {
+  const void* q;          /* row i of head g: q + i*q_row + g*q_head                    */
+  const void* k_cache;    /* [c] rows, cache_row apart (may be NULL when c == 0)        */
+  const void* v_cache;
+  const void* k_chunk;    /* [m] rows, chunk_row apart (may be NULL when m == 0)        */
+  const void* v_chunk;
+  void* out;              /* row i of head g: out + i*out_row + g*out_head              */
+  float* lse;             /* [G*n_que] natural log of the sums, row g*n_que + i; or NULL */
+  const uint8_t* k_scale; /* [ceil(c / block)] of an 8-bit cache; or NULL               */
+  const uint8_t* v_scale;
+  const int32_t* m_live;  /* device; or NULL                                            */
+  int64_t q_row, q_head, out_row, out_head, cache_row, chunk_row;
+  int32_t n_que;          /* rows per query head, >= 0                                  */
+  int32_t c, m;           /* >= 0                                                       */
+  int32_t causal;         /* 0 or 1                                                     */
+} finch_attention;
+
+/* Bytes of workspace of finch_attend on this batch (0: none is needed). */
+finch_status finch_attend_workspace_size(const finch_ctx* ctx, const finch_attention* host_desc, int32_t n_problems,
+                                         size_t* bytes);
+finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, const finch_attention* dev_desc,
+                          int32_t n_problems, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Measurement helpers (not part of the method).  finch_profile(ctx, 1) creates a
  * pool of HIP events (this call allocates; make it outside any timed loop) and

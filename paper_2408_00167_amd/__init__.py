@@ -1,7 +1,8 @@
 """Python binding of libfinch.so (the C ABI declared in include/finch.h).
 
-Argument marshalling only: every step of the path (scoring, top-r, compaction)
-runs in the HIP kernels behind the C ABI.  There is no CPU or PyTorch fallback: if
+Argument marshalling only: every step of the path (scoring, top-r, compaction), and of what
+stands around it in a layer (rotation, attention, 8-bit caches), runs in the HIP kernels behind
+the C ABI.  There is no CPU or PyTorch fallback: if
 the shared library is missing or no GPU is usable, the calls raise.
 
 PyTorch is used for device memory and streams: tensors supply device pointers,
@@ -35,7 +36,8 @@ EXPORTED_SYMBOLS = (
     "finch_status_string", "finch_version", "finch_profile", "finch_profile_read",
     "finch_set_option", "finch_set_reposition", "finch_prompt_lse", "finch_loop", "finch_loop_workspace_size",
     "finch_step_static", "finch_static_scratch_bytes", "finch_loop_check",
-    "finch_workspace_status",
+    "finch_workspace_status", "finch_rotate", "finch_rope_frequencies", "finch_quantize", "finch_attend",
+    "finch_attend_workspace_size",
 )
 
 KERNEL_NAMES = ("rowstats", "lse", "colsum", "select", "gather", "owner", "prompt_lse")
@@ -44,12 +46,14 @@ FINCH_OPT_STEP_PATH = 1
 FINCH_OPT_SLICE_KEYS = 3
 FINCH_OPT_LAYER_GROUP = 4
 FINCH_OPT_LAYER_WAIT_TICKS = 5
+FINCH_OPT_SCALE_BLOCK = 6
 FINCH_SCHEDULE_PROPORTIONAL, FINCH_SCHEDULE_CONSTANT = 0, 1
 FINCH_PATH_AUTO = 0
 FINCH_PATH_SEPARATE = 1
 FINCH_PATH_OWNER = 3
 FINCH_ROPE_OFF, FINCH_ROPE_HALF, FINCH_ROPE_INTERLEAVED = 0, 1, 2
 FINCH_ORDER_ASCENDING, FINCH_ORDER_RANK = 0, 1
+FINCH_SCALING_NONE, FINCH_SCALING_LINEAR, FINCH_SCALING_BANDED, FINCH_SCALING_RAMP = 0, 1, 2, 3
 
 
 class FinchError(RuntimeError):
@@ -75,6 +79,38 @@ class finch_problem(ctypes.Structure):
                 ("n_que", ctypes.c_int32), ("c", ctypes.c_int32), ("m", ctypes.c_int32),
                 ("r", ctypes.c_int32), ("k_que", ctypes.c_void_p), ("lse_extra", ctypes.c_void_p),
                 ("q_doc", ctypes.c_void_p)]
+
+
+_ROWS_STRIDES = ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head",
+                 "q_out_row", "q_out_head", "k_out_row", "k_out_head", "v_out_row", "v_out_head")
+
+
+class finch_rows(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out", "k_out", "v_out", "pos", "slot")] +
+                [(n, ctypes.c_int64) for n in _ROWS_STRIDES] +
+                [(n, ctypes.c_int32) for n in ("n", "kv_heads", "pos0", "slots")])
+
+
+class finch_rotary(ctypes.Structure):
+    _fields_ = [("pairing", ctypes.c_int32), ("dims", ctypes.c_int32), ("freq", ctypes.c_void_p),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float), ("gain", ctypes.c_float)]
+
+
+class finch_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("reserved", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("context", ctypes.c_double)]
+
+
+class finch_quantization(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_out", "v_out", "k_scale", "v_scale")] +
+                [("in_row", ctypes.c_int64), ("out_row", ctypes.c_int64), ("n", ctypes.c_int32), ("reserved", ctypes.c_int32)])
+
+
+class finch_attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "k_chunk", "v_chunk", "out", "lse", "k_scale", "v_scale",
+                                                "m_live")] +
+                [(n, ctypes.c_int64) for n in ("q_row", "q_head", "out_row", "out_head", "cache_row", "chunk_row")] +
+                [(n, ctypes.c_int32) for n in ("n_que", "c", "m", "causal")])
 
 
 _lib = None
@@ -132,6 +168,16 @@ def load_library() -> ctypes.CDLL:
     lib.finch_loop_check.restype = ctypes.c_int
     lib.finch_set_option.argtypes = [vp, i32, i64]
     lib.finch_set_option.restype = ctypes.c_int
+    lib.finch_rotate.argtypes = [vp, P(finch_rotary), P(finch_rows), vp, i32, vp]
+    lib.finch_rotate.restype = ctypes.c_int
+    lib.finch_rope_frequencies.argtypes = [i32, ctypes.c_double, P(finch_rope_scaling), P(ctypes.c_double), i32, P(ctypes.c_float)]
+    lib.finch_rope_frequencies.restype = ctypes.c_int
+    lib.finch_quantize.argtypes = [vp, P(finch_quantization), vp, i32, vp]
+    lib.finch_quantize.restype = ctypes.c_int
+    lib.finch_attend_workspace_size.argtypes = [vp, P(finch_attention), i32, P(sz)]
+    lib.finch_attend_workspace_size.restype = ctypes.c_int
+    lib.finch_attend.argtypes = [vp, P(finch_attention), vp, i32, vp, sz, vp]
+    lib.finch_attend.restype = ctypes.c_int
     lib.finch_version.argtypes = []
     lib.finch_version.restype = i32
     _lib = lib
@@ -262,6 +308,36 @@ def finch_loop_check(dtype: int, head_dim: int, group_size: int, host_desc, host
     return int(load_library().finch_loop_check(ctypes.byref(cfg), host_desc, host_step_first, n_steps))
 
 
+def finch_rotate(ctx, how: finch_rotary, host_desc, dev_desc_ptr: int, n: int, stream: int = 0) -> None:
+    _check(load_library().finch_rotate(ctx, ctypes.byref(how), host_desc, ctypes.c_void_p(dev_desc_ptr), n,
+                                       ctypes.c_void_p(stream)), "finch_rotate", ctx)
+
+
+def finch_rope_frequencies(dims: int, base: float = 10000.0, kind: int = FINCH_SCALING_NONE, factor: float = 1.0,
+                           low: float = 0.0, high: float = 0.0, context: float = 0.0):
+    """(radians per position of the dims / 2 channel pairs, the gain that goes with them)."""
+    scaling = finch_rope_scaling(kind, 0, factor, low, high, context)
+    freq, gain = (ctypes.c_double * max(1, dims // 2))(), ctypes.c_float(1.0)
+    _check(load_library().finch_rope_frequencies(dims, base, ctypes.byref(scaling), freq, max(0, dims // 2), ctypes.byref(gain)),
+           "finch_rope_frequencies")
+    return list(freq[:dims // 2]), float(gain.value)
+
+
+def finch_quantize(ctx, host_desc, dev_desc_ptr: int, n: int, stream: int = 0) -> None:
+    _check(load_library().finch_quantize(ctx, host_desc, ctypes.c_void_p(dev_desc_ptr), n, ctypes.c_void_p(stream)),
+           "finch_quantize", ctx)
+
+
+def finch_attend_workspace_size(ctx, host_desc, n: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().finch_attend_workspace_size(ctx, host_desc, n, ctypes.byref(out)), "finch_attend_workspace_size", ctx)
+    return out.value
+
+
+def finch_attend(ctx, host_desc, dev_desc_ptr: int, n: int, ws_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _call("finch_attend", ctx, host_desc, dev_desc_ptr, n, ws_ptr, ws_bytes, stream)
+
+
 def finch_version() -> int:
     return load_library().finch_version()
 
@@ -321,6 +397,201 @@ class LoopBatch:
         self.dev_first = torch.tensor(first, dtype=torch.int32, device=device)
 
 
+def _upload(host, n: int, struct, device):
+    import torch
+    raw = bytes(host)[: n * ctypes.sizeof(struct)]
+    return torch.frombuffer(bytearray(raw if raw else b"\0" * 8), dtype=torch.uint8).to(device)
+
+
+def _rows_of(t, dims: int, what: str):
+    """A tensor whose last dimension lies element after element, or a ValueError."""
+    if t.dim() != dims:
+        raise ValueError(f"{what}: {t.dim()} dimensions, want {dims}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the channels of a head must lie one after the other")
+    return t
+
+
+def _flat(t, n: int, dtype, what: str):
+    """Device pointer of a contiguous tensor of at least n elements of one type (None: none)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{what}: want {n} contiguous elements of {dtype}")
+    return t.data_ptr() if t.numel() else None
+
+
+def _same(ts, what: str):
+    a = ts[0]
+    for t in ts[1:]:
+        if t.dtype != a.dtype or t.shape[-1] != a.shape[-1]:
+            raise ValueError(f"{what}: types and channels must agree")
+
+
+class Rotary:
+    """What `Finch.rotate` does to queries and keys: pairing, rotated channels, frequencies ([dims / 2] float64 on the
+    device: see finch_rope_frequencies), gain, and the weights of a norm per head ([head_dim])."""
+
+    def __init__(self, pairing: int = FINCH_ROPE_HALF, dims: int = 0, freq=None, gain: float = 1.0, q_norm=None, k_norm=None,
+                 eps: float = 1e-6):
+        import torch
+        self.tensors = (freq, q_norm, k_norm)  # kept alive
+        self.norm = next((w for w in (q_norm, k_norm) if w is not None), None)
+        for w in (q_norm, k_norm):
+            if w is not None and (w.dtype != self.norm.dtype or w.dim() != 1 or w.shape != self.norm.shape or not w.is_contiguous()):
+                raise ValueError("norm weights: want one contiguous [head_dim] tensor each, of one type")
+        self.struct = finch_rotary(pairing, dims, _flat(freq, dims // 2, torch.float64, "freq"), _ptr(q_norm), _ptr(k_norm), eps, gain)
+
+
+class RowsBatch:
+    """Descriptors of `Finch.rotate`.  `requests` is a sequence of dicts with tensors q [n][G * kv_heads][d], k and v
+    [n][kv_heads][d] (each may be None; views of a packed projection will do), q_out, k_out, v_out of the same layout, and
+    optionally int32 `pos` [n] and `slot` [n] (rows of k_out and v_out), or an int `pos0`."""
+
+    def __init__(self, requests: Sequence[Dict], device="cuda"):
+        import torch
+        self.n = len(requests)
+        self.host = (finch_rows * max(1, self.n))()
+        self.key = None  # (dtype, channels, query heads per KV head or None)
+        for i, r in enumerate(requests):
+            d = self.host[i]
+            parts = {name: r.get(name) for name in ("q", "k", "v")}
+            given = {name: t for name, t in parts.items() if t is not None}
+            if not given:
+                raise ValueError("a request needs q, k or v")
+            _same(list(given.values()) + [r[name + "_out"] for name in given], "rows")
+            d.n = next(iter(given.values())).shape[0]
+            slot = r.get("slot")
+            for name, t in given.items():
+                out = _rows_of(r[name + "_out"], 3, name + "_out")
+                _rows_of(t, 3, name)
+                room = out.shape[0]
+                if t.shape[0] != d.n or t.shape[1] != out.shape[1] or (room != d.n and (slot is None or name == "q")):
+                    raise ValueError(f"{name}: {tuple(t.shape)} and {tuple(out.shape)} do not go together")
+                for at, x in ((name, t), (name + "_out", out)):
+                    setattr(d, at, x.data_ptr() if x.numel() else None)
+                    setattr(d, at + "_row", x.stride(0) if x.shape[0] > 1 else 0)
+                    setattr(d, at + "_head", x.stride(1) if x.shape[1] > 1 else 0)
+            heads = [given[name].shape[1] for name in ("k", "v") if name in given]
+            group = None
+            if heads:
+                d.kv_heads = heads[0]
+                if heads[-1] != heads[0] or ("q" in given and given["q"].shape[1] % heads[0]):
+                    raise ValueError("k and v need as many heads, q a multiple of that")
+                group = given["q"].shape[1] // heads[0] if "q" in given else None
+            else:
+                d.kv_heads = int(r["kv_heads"])
+                if d.kv_heads < 1 or given["q"].shape[1] % d.kv_heads:
+                    raise ValueError("q needs a multiple of kv_heads heads")
+                group = given["q"].shape[1] // d.kv_heads
+            d.pos, d.pos0 = _flat(r.get("pos"), d.n, torch.int32, "pos"), int(r.get("pos0", 0))
+            if slot is not None:
+                rooms = {r[name + "_out"].shape[0] for name in ("k", "v") if name in given}
+                if len(rooms) > 1:
+                    raise ValueError("k_out and v_out need as many rows")
+                d.slot, d.slots = _flat(slot, d.n, torch.int32, "slot"), rooms.pop() if rooms else 0
+            first = next(iter(given.values()))
+            key = (first.dtype, first.shape[-1], group if group is not None else (self.key[2] if self.key else None))
+            if self.key and (key[:2] != self.key[:2] or (self.key[2] is not None and key[2] != self.key[2])):
+                raise ValueError("requests of one batch: types, channels and heads per group must agree")
+            self.key = key
+        self.dev = _upload(self.host, self.n, finch_rows, device)
+        self.dev_ptr = self.dev.data_ptr()
+
+
+class QuantizeBatch:
+    """Descriptors of `Finch.quantize`: dicts with k, v [n][d], k_out, v_out [n][d] (float8_e4m3fn or uint8), k_scale, v_scale
+    (uint8, one per block of rows)."""
+
+    def __init__(self, problems: Sequence[Dict], device="cuda"):
+        import torch
+        self.n = len(problems)
+        self.host = (finch_quantization * max(1, self.n))()
+        self.key, self.min_block = None, 1
+        for i, pb in enumerate(problems):
+            d = self.host[i]
+            k, v, ko, vo = (_rows_of(pb[name], 2, name) for name in ("k", "v", "k_out", "v_out"))
+            _same([k, v], "k, v")
+            if k.shape != v.shape or ko.shape != k.shape or vo.shape != k.shape:
+                raise ValueError("k, v, k_out and v_out need one shape")
+            if k.shape[0] > 1 and (k.stride(0) != v.stride(0) or ko.stride(0) != vo.stride(0)):
+                raise ValueError("k and v, and k_out and v_out, need the same distance between rows")
+            if any(t.dtype not in (torch.uint8, torch.float8_e4m3fn) for t in (ko, vo)):
+                raise ValueError("k_out, v_out: want uint8 or float8_e4m3fn")
+            d.n = k.shape[0]
+            d.in_row, d.out_row = k.stride(0), ko.stride(0)
+            if d.n == 1:
+                d.in_row = d.out_row = k.shape[1]
+            for name, t in (("k", k), ("v", v), ("k_out", ko), ("v_out", vo)):
+                setattr(d, name, t.data_ptr() if t.numel() else None)
+            for name in ("k_scale", "v_scale"):
+                setattr(d, name, _flat(pb[name], 1 if d.n else 0, torch.uint8, name))
+                if d.n:
+                    self.min_block = max(self.min_block, -(-d.n // pb[name].numel()))
+            key = (k.dtype, k.shape[1], None)
+            if self.key not in (None, key):
+                raise ValueError("problems of one batch: types and channels must agree")
+            self.key = key
+        self.dev = _upload(self.host, self.n, finch_quantization, device)
+        self.dev_ptr = self.dev.data_ptr()
+
+
+class AttentionBatch:
+    """Descriptors of `Finch.attend`: dicts with q and out [n_que][G][d], k_cache, v_cache [c][d], k_chunk, v_chunk [m][d] (pairs
+    may be None), and optionally lse ([G * n_que] float32), k_scale and v_scale (uint8; the cache rows are then e4m3 bytes, float8_e4m3fn
+    or uint8), m_live (one int32), causal (default True).  The tensors are only read for their device pointers and strides."""
+
+    def __init__(self, problems: Sequence[Dict], device="cuda"):
+        import torch
+        self.n = len(problems)
+        self.host = (finch_attention * max(1, self.n))()
+        self.key, self.min_block, self.planned = None, 1, None
+        for i, pb in enumerate(problems):
+            d = self.host[i]
+            q, out = _rows_of(pb["q"], 3, "q"), _rows_of(pb["out"], 3, "out")
+            if q.shape != out.shape or q.dtype != out.dtype:
+                raise ValueError("q and out need one shape and type")
+            d.n_que, group = q.shape[0], q.shape[1]
+            d.q_row, d.q_head, d.out_row, d.out_head = q.stride(0), q.stride(1), out.stride(0), out.stride(1)
+            if d.n_que == 1:
+                d.q_row, d.out_row = q.shape[2], out.shape[2]
+            if group == 1:
+                d.q_head, d.out_head = q.shape[2], out.shape[2]
+            d.q, d.out = (t.data_ptr() if t.numel() else None for t in (q, out))
+            eight = pb.get("k_scale") is not None or pb.get("v_scale") is not None
+            for part, count in (("cache", "c"), ("chunk", "m")):
+                k, v = pb.get("k_" + part), pb.get("v_" + part)
+                if (k is None) != (v is None):
+                    raise ValueError(f"k_{part} and v_{part}: both or neither")
+                if k is None:
+                    continue
+                _rows_of(k, 2, "k_" + part), _rows_of(v, 2, "v_" + part)
+                if k.shape != v.shape or k.dtype != v.dtype or k.shape[1] != q.shape[2] or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+                    raise ValueError(f"k_{part} and v_{part}: shapes, types and distances of rows must agree")
+                bytes8 = eight and part == "cache"
+                if k.dtype not in ((torch.uint8, torch.float8_e4m3fn) if bytes8 else (q.dtype,)):
+                    raise ValueError(f"k_{part}: rows of {k.dtype}")
+                setattr(d, count, k.shape[0])
+                setattr(d, part + "_row", k.stride(0) if k.shape[0] > 1 else k.shape[1])
+                setattr(d, "k_" + part, k.data_ptr() if k.numel() else None)
+                setattr(d, "v_" + part, v.data_ptr() if v.numel() else None)
+            if eight:
+                for name in ("k_scale", "v_scale"):
+                    if pb.get(name) is None:
+                        raise ValueError("k_scale and v_scale: both or neither")
+                    setattr(d, name, _flat(pb[name], 1, torch.uint8, name))
+                    self.min_block = max(self.min_block, -(-d.c // pb[name].numel()))
+            d.lse = _flat(pb.get("lse"), group * d.n_que, torch.float32, "lse")
+            d.m_live = _flat(pb.get("m_live"), 1, torch.int32, "m_live")
+            d.causal = 1 if pb.get("causal", True) else 0
+            key = (q.dtype, q.shape[2], group)
+            if self.key not in (None, key):
+                raise ValueError("problems of one batch: types, channels and heads per group must agree")
+            self.key = key
+        self.dev = _upload(self.host, self.n, finch_attention, device)
+        self.dev_ptr = self.dev.data_ptr()
+
+
 class Finch:
     """A context plus a workspace tensor that grows on demand (outside any timed
     or captured region the caller should pre-size it with `reserve`)."""
@@ -332,6 +603,8 @@ class Finch:
         self.device = torch.device(device)
         self.ctx = finch_create(dtype, head_dim, group_size)
         self.ws = None
+        self.key = (torch.bfloat16 if dtype == FINCH_BF16 else torch.float32, head_dim, group_size)
+        self.scale_block = 64
 
     def close(self):
         if self.ctx is not None:
@@ -421,3 +694,46 @@ class Finch:
         s = torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
         finch_loop(self.ctx, lb.batch.host, lb.batch.dev_ptr, lb.host_first, lb.dev_first.data_ptr(),
                    lb.n_steps, self.ws.data_ptr(), self.ws.numel(), s)
+
+    def set_scale_block(self, rows: int) -> None:
+        """Rows that share a power of two in 8-bit caches (16, 32, 64 or 128)."""
+        finch_set_option(self.ctx, FINCH_OPT_SCALE_BLOCK, rows)
+        self.scale_block = rows
+
+    def _suits(self, key, what: str) -> None:
+        """A batch built of tensors of another type or shape than the context's would be misread."""
+        if key is not None and (key[:2] != self.key[:2] or key[2] not in (None, self.key[2])):
+            raise ValueError(f"{what}: batch of {key}, context of {self.key}")
+
+    def _stream(self, stream):
+        import torch
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
+
+    def rotate(self, batch: RowsBatch, how: Rotary, stream=None):
+        """Norm, rotary embedding and placing of projected rows."""
+        self._suits(batch.key, "rotate")
+        if how.norm is not None and (how.norm.dtype, how.norm.shape[0]) != self.key[:2]:
+            raise ValueError("rotate: norm weights of another type or size than the context's heads")
+        finch_rotate(self.ctx, how.struct, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
+
+    def quantize(self, batch: QuantizeBatch, stream=None):
+        """Rows of K and V as e4m3 with one power of two per block of rows."""
+        self._suits(batch.key, "quantize")
+        if batch.min_block > self.scale_block:
+            raise ValueError("quantize: too few scales for blocks of this size")
+        finch_quantize(self.ctx, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
+
+    def reserve_attend(self, batch: AttentionBatch) -> int:
+        need = finch_attend_workspace_size(self.ctx, batch.host, batch.n)
+        self._grow(need)
+        batch.planned = (self, need)
+        return need
+
+    def attend(self, batch: AttentionBatch, stream=None):
+        """Attention over [cache ; chunk]."""
+        self._suits(batch.key, "attend")
+        if batch.min_block > self.scale_block:
+            raise ValueError("attend: too few scales for blocks of this size")
+        if batch.planned is None or batch.planned[0] is not self or self.ws is None or self.ws.numel() < batch.planned[1]:
+            self.reserve_attend(batch)
+        finch_attend(self.ctx, batch.host, batch.dev_ptr, batch.n, self.ws.data_ptr(), self.ws.numel(), self._stream(stream))

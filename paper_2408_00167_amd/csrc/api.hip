@@ -10,35 +10,7 @@
 #include <new>
 #include <vector>
 
-#include "finch_internal.h"
-
-struct finch_ctx {
-  finch_config cfg;
-  int device;
-  size_t max_lds;   // largest dynamic LDS a workgroup may ask for
-  int last_hip;     // hipError_t of the last failed HIP call
-  int row_bytes;    // bytes of one K or V row
-  // optional per-kernel timing (finch_profile): pairs of events around launches
-  bool prof_on;
-  int prof_used;
-  hipEvent_t* prof_ev;   // 2 * kProfPairs events, or nullptr
-  int* prof_kind;        // kernel class of each pair
-  int n_cu;              // compute units of the device
-  int step_path;         // FINCH_PATH_AUTO / _SEPARATE / _OWNER
-  int slice_keys;        // target keys per workgroup slice of the bf16 scoring kernels
-  finch_reposition repos;  // {OFF, ASCENDING}: plain copies
-  int layer_group;         // > 1: runs of that many problems share one selection
-  int64_t layer_wait_ticks;  // bound of a workgroup's wait for its layer, 100 MHz ticks
-  int32_t* meet;             // meeting words of this context's launches with several workgroups per problem
-  void* static_scratch;    // this device's copy of the file-scope scratch array (finch_step_static)
-  int32_t* static_meet;    // and of the meeting words that go with it
-  // finch_loop: fingerprint of the last descriptor set whose slots were found free of
-  // overlaps (the check is repeated only when the descriptors change)
-  uint64_t loop_checked_hash;
-  bool loop_checked;
-  bool loop_rows_may_stay;  // what check_slot_overlaps said of that set
-  int32_t* loop_ways;       // LaunchParams::ways of its whole loops
-};
+#include "context.h"
 
 // Scratch of finch_step_static: the workspace of a step, held by the library itself so
 // that the call neither takes a workspace nor allocates.  Every GPU the library runs on
@@ -50,6 +22,10 @@ static __device__ __align__(256) int32_t scratch_meet[finch::kClusterMeetWords];
 namespace {
 
 using finch::LaunchParams;
+using finch::align_up;
+using finch::aligned;
+using finch::hip_fail;
+using finch::overlaps;
 
 enum Need : unsigned {
   kNeedQK = 1u,      // q, k_cache, k_chunk are read
@@ -77,15 +53,6 @@ struct Plan {
   size_t off_stats = 0, off_lse = 0, off_scores = 0, off_layer = 0, off_sync = 0, total = 0;
   int32_t sync_words = 0;  // counters of the layer runs (workspace word 0 is the status word)
 };
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  if (!a || !b || na == 0 || nb == 0) return false;
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + nb && b0 < a0 + na;
-}
 
 size_t score_lds(const finch_ctx* ctx, int row_chunk) {
   const size_t d = static_cast<size_t>(ctx->cfg.head_dim);
@@ -301,11 +268,6 @@ LaunchParams make_params(const finch_ctx* ctx, const finch_problem* dd, int32_t 
   p.layer_err = reinterpret_cast<int32_t*>(base);
   p.spin_ticks = ctx->layer_wait_ticks;
   return p;
-}
-
-finch_status hip_fail(finch_ctx* ctx, hipError_t e) {
-  ctx->last_hip = static_cast<int>(e);
-  return FINCH_ERR_HIP;
 }
 
 // Device addresses of `scratch` and `scratch_meet` on each GPU.  In host code an array's name
@@ -924,6 +886,7 @@ finch_status finch_create(const finch_config* cfg, finch_ctx** out) {
   ctx->loop_checked_hash = 0;
   ctx->loop_rows_may_stay = false;
   ctx->loop_ways = nullptr;
+  ctx->scale_block = 64;
   ctx->meet = nullptr;
   hipError_t e = hipGetDevice(&ctx->device);
   StaticAddresses a = {nullptr, nullptr, nullptr};
@@ -993,6 +956,10 @@ finch_status finch_set_option(finch_ctx* ctx, int32_t option, int64_t value) {
     case FINCH_OPT_SLICE_KEYS:
       if (value < 256 || value > (1 << 24)) return FINCH_ERR_INVALID_ARG;
       ctx->slice_keys = static_cast<int>(value);
+      return FINCH_OK;
+    case FINCH_OPT_SCALE_BLOCK:
+      if (value != 16 && value != 32 && value != 64 && value != 128) return FINCH_ERR_INVALID_ARG;
+      ctx->scale_block = static_cast<int>(value);
       return FINCH_OK;
     default:
       return FINCH_ERR_INVALID_ARG;
@@ -1356,6 +1323,6 @@ const char* finch_status_string(finch_status s) {
   return "unknown status";
 }
 
-int32_t finch_version(void) { return 100; }
+int32_t finch_version(void) { return 200; }
 
 }  // extern "C"

@@ -1,0 +1,371 @@
+// Attention of few rows over many keys, bf16: out = softmax(Q K^T / sqrt(d)) V for 32 stacked rows
+// a workgroup, each of whose four waves takes tiles of 32 keys of its own through the whole
+// calculation with a running softmax; the waves' results are joined in LDS, those of several
+// workgroups on the same rows by attend_join.  A generated token's pass is bound by the bytes of
+// the cache, so every row of K and V is read from HBM once, straight into registers.
+//
+// S^T = K Q^T is one chain of v_mfma_f32_32x32x16_bf16 per tile: K rows are the A operand as they
+// lie in memory, and a lane ends up with 16 keys of one row, whose maximum and sum are the
+// lane's own but for one exchange with the lane 32 further on.  O^T = V^T P^T takes exactly those
+// weights as its B operand if the 16 keys of a step are numbered as the lanes hold them (lane half h:
+// keys 4h..4h+3 and 8+4h..8+4h+3), and V^T as the A operand: V goes through 8 KB of LDS of the
+// wave's own and comes out transposed by ds_read_b64_tr_b16.  Pieces of 16 bytes are swapped
+// by row so that neither side of that meets bank conflicts.  In O^T a lane has one row, so moving
+// the softmax's reference is a multiplication by one number a lane.
+//
+// K of the next tile is under way while the softmax runs, V of the next tile during P V.
+#include "attend.h"
+
+namespace finch {
+
+namespace {
+
+typedef __attribute__((address_space(3))) s16x4* lds_tr;
+
+// rows of K or V in memory
+struct Part {
+  const char* k;
+  const char* v;
+  long long row;  // bytes
+  int n;          // rows
+  const unsigned char* ks;
+  const unsigned char* vs;
+};
+
+template <int D, bool E8>
+struct Tile {
+  static constexpr int kPieces = D / (E8 ? 32 : 16);  // 16-byte pieces a lane has of K, and of V
+  u32x4 k[kPieces], v[kPieces];
+  unsigned ks, vs[kPieces];
+};
+
+// Lane (t, h) takes of key t, for the pair of k-steps u, channels 32u + 16h .. +15: 16 bytes of e4m3 or two pieces
+// of bf16.  (Any order of the channels will do, as long as Q is read in the same.)
+template <int D, bool E8>
+__device__ __forceinline__ void load_k(Tile<D, E8>& t, const Part& a, int key0, int shift, int lane) {
+  const int key = min(key0 + (lane & 31), a.n - 1);
+  const FINCH_GLOBAL u32x4* rp = as_global<u32x4>(a.k + key * a.row + (lane >> 5) * (E8 ? 16 : 32));
+  if (E8) {
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) t.k[u] = rp[2 * u];
+    t.ks = as_global<unsigned char>(a.ks)[key >> shift];
+  } else {
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) {
+      t.k[2 * u] = rp[4 * u];
+      t.k[(2 * u + 1) % Tile<D, E8>::kPieces] = rp[4 * u + 1];
+    }
+  }
+}
+
+template <int D, bool E8>
+__device__ __forceinline__ void load_v(Tile<D, E8>& t, const Part& a, int key0, int shift, int lane) {
+  constexpr int kPer = D / (E8 ? 16 : 8);  // pieces of a row
+#pragma unroll
+  for (int i = 0; i < Tile<D, E8>::kPieces; ++i) {
+    const int id = i * 64 + lane, key = min(key0 + id / kPer, a.n - 1);
+    t.v[i] = as_global<u32x4>(a.v + key * a.row)[id % kPer];
+    if (E8) t.vs[i] = as_global<unsigned char>(a.vs)[key >> shift];
+  }
+}
+
+// 8 e4m3 numbers times 2^(e - 127) as bf16: exact, one instruction for two.
+__device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi, unsigned e) {
+  const float f = __uint_as_float(e << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Which piece of row r takes the place of piece 0 in LDS: rows 0..7 (0..3 with 64 channels) differ by two pieces.
+template <int D>
+__device__ __forceinline__ int swap_of(int r) {
+  return 2 * (r & (D == 128 ? 7 : 3));
+}
+
+template <int D, bool E8>
+__device__ __forceinline__ void v_to_lds(const Tile<D, E8>& t, char* lds, int lane) {
+  constexpr int kPer = D / (E8 ? 16 : 8);
+#pragma unroll
+  for (int i = 0; i < Tile<D, E8>::kPieces; ++i) {
+    const int id = i * 64 + lane, r = id / kPer, pc = id % kPer;
+    char* row = lds + r * (2 * D);
+    if (E8) {
+      *reinterpret_cast<bf16x8*>(row + ((2 * pc) ^ swap_of<D>(r)) * 16) = widen(t.v[i][0], t.v[i][1], t.vs[i]);
+      *reinterpret_cast<bf16x8*>(row + ((2 * pc + 1) ^ swap_of<D>(r)) * 16) = widen(t.v[i][2], t.v[i][3], t.vs[i]);
+    } else {
+      *reinterpret_cast<u32x4*>(row + (pc ^ swap_of<D>(r)) * 16) = t.v[i];
+    }
+  }
+}
+
+// The rows' state in a lane: reference (log2 domain), sum of the lane's weights, O^T.
+template <int D>
+struct Rows {
+  float ref = -kInf, sum = 0.f;
+  f32x16 o[D / 32];
+};
+
+// Tiles first, first + step, ... below last of one part (or, for bf16, of both one after the other).
+template <int D, bool E8>
+__device__ __forceinline__ void stream(Rows<D>& st, const bf16x8 (&q)[D / 16], const Part& cache, const Part& chunk, int cache_tiles,
+                                       int first, int last, int step, int lim, int lim_all, float scale, int shift, char* lds, int lane) {
+  if (first >= last) return;
+  const int h = lane >> 5;
+  Tile<D, E8> t;
+  const auto part = [&](int i) -> Part { return i < cache_tiles ? cache : chunk; };
+  const auto key0 = [&](int i) { return (i < cache_tiles ? i : i - cache_tiles) * kRowsKeys; };
+  // where a lane reads V^T: keys 4h + (lane & 15) / 4 of a step, columns of its 16-lane group
+  int off[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    const int key = 4 * h + ((lane & 15) >> 2), pc = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    off[db] = key * (2 * D) + (pc ^ swap_of<D>(key)) * 16 + 8 * (lane & 1);
+  }
+  load_k<D, E8>(t, part(first), key0(first), shift, lane);
+  load_v<D, E8>(t, part(first), key0(first), shift, lane);
+  for (int i = first; i < last; i += step) {
+    const int next = i + step < last ? i + step : i;  // (the last one again: a branch would hide how many loads are pending)
+    f32x16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) {
+      bf16x8 a, b;
+      if (E8) {
+        a = widen(t.k[u][0], t.k[u][1], t.ks);
+        b = widen(t.k[u][2], t.k[u][3], t.ks);
+      } else {
+        a = __builtin_bit_cast(bf16x8, t.k[2 * u]);
+        b = __builtin_bit_cast(bf16x8, t.k[(2 * u + 1) % Tile<D, E8>::kPieces]);
+      }
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[2 * u], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, q[2 * u + 1], s, 0, 0, 0);
+    }
+    load_k<D, E8>(t, part(next), key0(next), shift, lane);
+    // keys past the part's end or the row's limit; lim_all: what every row of the tile sees
+    const int base = key0(i), off_c = i < cache_tiles ? 0 : cache.n;
+    if (base + kRowsKeys > min(lim_all - off_c, part(i).n)) {
+      const int left = min(lim - off_c, part(i).n) - base;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = acc_key(v, h) < left ? s[v] : -kInf;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
+    mx = fmaxf(mx, other_half(mx)) * scale;
+    if (__any(mx > st.ref + kSlack)) {
+      const float ref = fmaxf(st.ref, mx);
+      const float f = st.ref == -kInf ? 0.f : fast_exp2(st.ref - ref);
+      st.ref = ref;
+      st.sum *= f;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) st.o[db][v] *= f;
+    }
+    const float ref = st.ref == -kInf ? 0.f : st.ref;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      s[v] = fast_exp2(fmaf(s[v], scale, -ref));
+      st.sum += s[v];
+    }
+    v_to_lds<D, E8>(t, lds, lane);
+    load_v<D, E8>(t, part(next), key0(next), shift, lane);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      bf16x8 pf;
+#pragma unroll
+      for (int v = 0; v < 8; ++v) pf[v] = static_cast<__bf16>(s[8 * b + v]);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b) * (2 * D)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b + 8) * (2 * D)));
+        const s16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf, st.o[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+template <int D, bool EIGHT>
+__global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams prm) {
+  // V of the waves' tiles; later three quarters of every wave's O^T
+  constexpr int kQuarter = D / 8;  // values of O^T a wave ends up with, per lane
+  __shared__ __align__(16) char lds[kRowsWaves * 3 * kQuarter * 64 * 4];
+  __shared__ float ml[2][kRowsWaves][kRowsTile];
+  static_assert(sizeof(lds) >= kRowsWaves * kRowsKeys * D * 2, "V tiles of all waves");
+  const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = rest % prm.row_tiles, split = rest / prm.row_tiles;
+  const Seen pb(prm, p);
+  const int r0 = rt * kRowsTile;
+  if (r0 >= pb.R) return;
+  const Share sh(prm, pb, r0, kRowsTile, kRowsKeys, split);
+  if (split >= sh.active) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), h = lane >> 5;
+  const int row = lane & 31, rr = min(r0 + row, pb.R - 1), tok = rr / pb.group, head = rr % pb.group;
+  bf16x8 q[D / 16];
+  {
+    const FINCH_GLOBAL u32x4* qp = as_global<u32x4>(static_cast<const char*>(pb.d.q) + (tok * pb.d.q_row + head * pb.d.q_head) * 2 + 32 * h);
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) {
+      q[2 * u] = __builtin_bit_cast(bf16x8, qp[4 * u]);
+      q[2 * u + 1] = __builtin_bit_cast(bf16x8, qp[4 * u + 1]);
+    }
+  }
+  const bool eight = EIGHT && pb.d.k_scale != nullptr;
+  const Part cache = {static_cast<const char*>(pb.d.k_cache), static_cast<const char*>(pb.d.v_cache), pb.d.cache_row * (eight ? 1 : 2), pb.d.c,
+                      pb.d.k_scale, pb.d.v_scale};
+  const Part chunk = {static_cast<const char*>(pb.d.k_chunk), static_cast<const char*>(pb.d.v_chunk), pb.d.chunk_row * 2, pb.m, nullptr, nullptr};
+  Rows<D> st;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) st.o[db][v] = 0.f;
+  const int lim = pb.limit(rr), lim_all = pb.limit(r0);
+  char* mine = lds + wave * (kRowsKeys * D * 2);
+  int first = sh.first + wave;
+  if (EIGHT && eight) {
+    const int end = min(sh.last, sh.cache_tiles);
+    stream<D, true>(st, q, cache, chunk, sh.cache_tiles, first, end, kRowsWaves, lim, lim_all, prm.scale_log2, prm.block_shift, mine, lane);
+    first = max(first, first + (end - first + kRowsWaves - 1) / kRowsWaves * kRowsWaves);
+  }
+  stream<D, false>(st, q, cache, chunk, sh.cache_tiles, first, sh.last, kRowsWaves, lim, lim_all, prm.scale_log2, prm.block_shift, mine, lane);
+
+  // join the waves: wave w ends up with values kQuarter * w .. of every lane's O^T
+  st.sum += other_half(st.sum);
+  if (h == 0) {
+    ml[0][wave][row] = st.ref;
+    ml[1][wave][row] = st.sum;
+  }
+  __syncthreads();
+  float top = ml[0][0][row];
+#pragma unroll
+  for (int w = 1; w < kRowsWaves; ++w) top = fmaxf(top, ml[0][w][row]);
+  float total = 0.f;
+#pragma unroll
+  for (int w = 0; w < kRowsWaves; ++w) total += top == -kInf ? 0.f : ml[1][w][row] * fast_exp2(ml[0][w][row] - top);
+  const float f = st.ref == -kInf ? 0.f : fast_exp2(st.ref - top);
+  float* ex = reinterpret_cast<float*>(lds);
+  float own[kQuarter];
+#pragma unroll
+  for (int w = 0; w < kRowsWaves; ++w) {
+    float* to = ex + (w * 3 + (wave < w ? wave : wave - 1)) * kQuarter * 64 + lane;
+#pragma unroll
+    for (int x = 0; x < kQuarter; ++x) {
+      const int v = w * kQuarter + x;
+      const float val = st.o[v >> 4][v & 15] * f;
+      if (w == wave) {
+        own[x] = val;
+      } else {
+        to[x * 64] = val;
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kQuarter; ++x) {
+    const float* from = ex + wave * 3 * kQuarter * 64 + x * 64 + lane;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) own[x] += from[w * kQuarter * 64];
+  }
+  if (r0 + row >= pb.R) return;
+  if (sh.active == 1) {
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    char* to = static_cast<char*>(pb.d.out) + (tok * pb.d.out_row + head * pb.d.out_head) * 2;
+#pragma unroll
+    for (int x = 0; x < kQuarter; x += 4) {
+      const int v = wave * kQuarter + x, d = 32 * (v >> 4) + 8 * ((v & 15) >> 2) + 4 * h;
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(own[x + e] * inv);
+      *as_global_mut<bf16x4>(to + 2 * d) = y;
+    }
+    if (pb.d.lse && wave == 0 && h == 0)
+      as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
+  } else {
+    const size_t at = ((static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits + split) * kRowsTile + row;
+    float* to = prm.part + at * D;
+#pragma unroll
+    for (int x = 0; x < kQuarter; x += 4) {
+      const int v = wave * kQuarter + x, d = 32 * (v >> 4) + 8 * ((v & 15) >> 2) + 4 * h;
+      *as_global_mut<f32x4>(to + d) = f32x4{own[x], own[x + 1], own[x + 2], own[x + 3]};
+    }
+    if (wave == 0 && h == 0) *as_global_mut<f32x2>(prm.part_ml + at) = f32x2{top, total};
+  }
+}
+
+// Joins the splits of a tile of rows: one workgroup for 32 of its rows (fewer if the tile has fewer).
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void attend_join(AttendParams prm, int tile_rows, int tile_keys, int chunks) {
+  const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, ch = rest % chunks, rt = rest / chunks;
+  const Seen pb(prm, p);
+  const int r0 = rt * tile_rows;
+  if (r0 + ch * 32 >= pb.R) return;
+  const Share sh(prm, pb, r0, tile_rows, tile_keys, 0);
+  if (sh.active == 1) return;
+  const int rows = min(min(32, tile_rows - ch * 32), pb.R - r0 - ch * 32);
+  for (int it = threadIdx.x; it < rows * (D / 4); it += 256) {
+    const int row = ch * 32 + it / (D / 4), pc = it % (D / 4);
+    const size_t at = (static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits * tile_rows + row;
+    const FINCH_GLOBAL f32x2* ml = as_global<f32x2>(prm.part_ml + at);
+    const FINCH_GLOBAL f32x4* o = as_global<f32x4>(prm.part + at * D) + pc;
+    float top = -kInf;
+    for (int s = 0; s < sh.active; ++s) top = fmaxf(top, ml[static_cast<size_t>(s) * tile_rows][0]);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < sh.active; ++s) {
+      const f32x2 w = ml[static_cast<size_t>(s) * tile_rows];
+      const float f = w[0] == -kInf ? 0.f : fast_exp2(w[0] - top);
+      const f32x4 y = o[static_cast<size_t>(s) * tile_rows * (D / 4)];
+      total += w[1] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+    }
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const int rr = r0 + row, tok = rr / pb.group, head = rr % pb.group;
+    const long long at_out = tok * pb.d.out_row + head * pb.d.out_head + 4 * pc;
+    if (BF16) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(sum[e] * inv);
+      *as_global_mut<bf16x4>(static_cast<char*>(pb.d.out) + 2 * at_out) = y;
+    } else {
+      *as_global_mut<f32x4>(static_cast<char*>(pb.d.out) + 4 * at_out) = f32x4{sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+    }
+    if (pb.d.lse && pc == 0) as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
+  }
+}
+
+hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * p.splits), block(64 * kRowsWaves);
+  if (head_dim == 128 && eight) {
+    hipLaunchKernelGGL((attend_rows<128, true>), grid, block, 0, s, p);
+  } else if (head_dim == 128) {
+    hipLaunchKernelGGL((attend_rows<128, false>), grid, block, 0, s, p);
+  } else if (eight) {
+    hipLaunchKernelGGL((attend_rows<64, true>), grid, block, 0, s, p);
+  } else {
+    hipLaunchKernelGGL((attend_rows<64, false>), grid, block, 0, s, p);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_join(int head_dim, bool bf16, int tile_rows, int tile_keys, const AttendParams& p, hipStream_t s) {
+  const int chunks = (tile_rows + 31) / 32;
+  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * chunks), block(256);
+  if (head_dim == 128 && bf16) {
+    hipLaunchKernelGGL((attend_join<128, true>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+  } else if (head_dim == 128) {
+    hipLaunchKernelGGL((attend_join<128, false>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+  } else if (bf16) {
+    hipLaunchKernelGGL((attend_join<64, true>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+  } else {
+    hipLaunchKernelGGL((attend_join<64, false>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace finch

@@ -1,0 +1,308 @@
+"""finch_attend against the definition in 64 bits (tests/layer_reference.py says where the bounds come from)."""
+import math
+
+import pytest
+import torch
+
+import paper_2408_00167_amd as F
+from tests import layer_reference as R
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def context():
+    made = {}
+
+    def get(dtype, d, G):
+        key = (dtype, d, G)
+        if key not in made:
+            made[key] = F.Finch(F.FINCH_BF16 if dtype == "bf16" else F.FINCH_F32, d, G)
+        made[key].set_scale_block(64)
+        return made[key]
+    yield get
+    for f in made.values():
+        f.close()
+
+
+def randn(gen, *shape, dtype=torch.bfloat16, scale=1.0):
+    return (torch.randn(*shape, generator=gen) * scale).to(dtype).cuda()
+
+
+def eight_bits(x, block):
+    """Rows as finch_quantize has them, made on the host."""
+    v, e = R.quantized(x, block)
+    t = R.e4m3_table()
+    code = torch.searchsorted(t, v.abs()) + 128 * (v < 0)
+    return code.to(torch.uint8).cuda(), torch.tensor([y + 127 for y in e] or [127], dtype=torch.uint8).cuda()
+
+
+def problem(gen, dtype, d, G, n, c, m, causal=True, eight=0, scale=1.0, lse=True):
+    """One problem on ordinary dense tensors, guarded by NaN rows and sentinels around everything."""
+    dt = DT[dtype]
+
+    def guarded(rows):  # rows of data with NaN before and behind
+        t = torch.full((rows + 16, d), math.nan, dtype=dt, device="cuda")
+        t[8:8 + rows] = randn(gen, rows, d, dtype=dt, scale=scale)
+        return t[8:8 + rows]
+    pb = dict(q=randn(gen, n, G, d, dtype=dt, scale=scale), k_chunk=guarded(m), v_chunk=guarded(m), causal=causal)
+    pb["full"] = torch.full((n + 2, G, d), 7.0, dtype=dt, device="cuda")
+    pb["out"] = pb["full"][1:n + 1]
+    if eight:
+        k, v = randn(gen, c, d, dtype=torch.float32, scale=scale), randn(gen, c, d, dtype=torch.float32, scale=scale)
+        for name, x in (("k", k), ("v", v)):
+            bytes8, pb[name + "_scale"] = eight_bits(x, eight)
+            t = torch.full((c + 16, d), 0x7F, dtype=torch.uint8, device="cuda")  # NaN
+            t[8:8 + c] = bytes8
+            pb[name + "_cache"] = t[8:8 + c]
+    else:
+        pb["k_cache"], pb["v_cache"] = guarded(c), guarded(c)
+    if lse:
+        pb["lse_full"] = torch.full((G * n + 2,), 7.0, device="cuda")
+        pb["lse"] = pb["lse_full"][1:G * n + 1]
+    return pb
+
+
+def candidates(pb, block=64, m=None):
+    k, v = pb["k_chunk"][:m], pb["v_chunk"][:m]
+    if "k_scale" in pb:
+        kc, vc = (R.dequantized(pb[n + "_cache"], pb[n + "_scale"], block) for n in ("k", "v"))
+    else:
+        kc, vc = R.host(pb["k_cache"]), R.host(pb["v_cache"])
+    return torch.cat([kc, R.host(k)]), torch.cat([vc, R.host(v)])
+
+
+def verify(pb, what, block=64, m=None):
+    k, v = candidates(pb, block, m)
+    R.check_attention(pb["out"], pb.get("lse"), pb["q"], k, v, pb["causal"], what)
+    assert bool((pb["full"][0] == 7).all()) and bool((pb["full"][-1] == 7).all()), f"{what}: rows around the output"
+    if "lse_full" in pb:
+        assert pb["lse_full"][0] == 7 and pb["lse_full"][-1] == 7, f"{what}: words around lse"
+
+
+SHAPES = [  # n_que, c, m
+    (1, 0, 1), (1, 1, 0), (1, 31, 1), (1, 32, 33), (1, 1408, 100), (2, 33, 2), (3, 100, 64), (5, 0, 5), (7, 65, 7), (33, 0, 33), (40, 10, 37),
+    (64, 129, 64), (130, 40, 130), (9, 257, 0), (4, 0, 2), (6, 2, 1)]
+
+
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("bf16", 64, 2), ("bf16", 128, 1), ("bf16", 128, 7), ("f32", 64, 1), ("f32", 128, 3)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_ragged_batch_of_all_shapes(context, dtype, d, G, causal):
+    fin, gen = context(dtype, d, G), torch.Generator().manual_seed(1)
+    pbs = [problem(gen, dtype, d, G, n, c, m, causal, lse=i % 3 != 2) for i, (n, c, m) in enumerate(SHAPES)]
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for s, pb in zip(SHAPES, pbs):
+        verify(pb, f"{dtype} d={d} G={G} causal={causal} {s}")
+
+
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("bf16", 64, 1), ("f32", 64, 4)])
+@pytest.mark.parametrize("shape", [(1, 5000, 1), (1, 0, 20000), (17, 3000, 17), (1, 40000, 3), (300, 70, 300)])
+def test_one_problem_split_over_the_chip(context, dtype, d, G, shape):
+    fin, gen = context(dtype, d, G), torch.Generator().manual_seed(2)
+    pb = problem(gen, dtype, d, G, *shape)
+    fin.attend(F.AttentionBatch([pb]))
+    torch.cuda.synchronize()
+    verify(pb, f"{dtype} d={d} G={G} {shape}")
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 3), (128, 1)])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+def test_eight_bit_caches(context, d, G, block):
+    fin, gen = context("bf16", d, G), torch.Generator().manual_seed(3)
+    fin.set_scale_block(block)
+    shapes = [(1, 1, 1), (1, 15, 0), (1, 64, 1), (1, 129, 30), (1, 2500, 77), (3, 200, 9), (40, 100, 40), (70, 300, 70), (5, 0, 5), (4, 3, 0)]
+    pbs = [problem(gen, "bf16", d, G, n, c, m, eight=block) for n, c, m in shapes]
+    pbs.append(problem(gen, "bf16", d, G, 1, 333, 20))  # and one whose cache is not in 8 bits
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for s, pb in zip(shapes + [(1, 333, 20)], pbs):
+        verify(pb, f"8 bits d={d} G={G} block={block} {s}", block)
+
+
+def test_large_and_masked_logits(context):
+    """Logits of several hundred, far ones first: the reference has to move, and weights far below vanish; and rows in which
+    every key has the same logit."""
+    fin, gen = context("bf16", 128, 2), torch.Generator().manual_seed(4)
+    pb = problem(gen, "bf16", 128, 2, 20, 500, 20, scale=6.0)
+    pb["k_cache"][:300] *= -1
+    for i in range(0, 500, 50):  # ever larger keys
+        pb["k_cache"][i] = pb["q"][0, 0] * (1 + i / 200)
+    flat = problem(gen, "bf16", 128, 2, 3, 200, 3)
+    flat["k_cache"].copy_(flat["k_cache"][:1].expand(200, -1).clone())
+    flat["k_chunk"].copy_(flat["k_cache"][:1].expand(3, -1).clone())
+    low = problem(gen, "bf16", 128, 2, 2, 100, 2)
+    low["q"].fill_(16.0)
+    low["k_cache"].fill_(-64.0)  # all logits -11585
+    low["k_chunk"].fill_(-64.0)
+    fin.attend(F.AttentionBatch([pb, flat, low]))
+    torch.cuda.synchronize()
+    for x, what in ((pb, "large"), (flat, "equal"), (low, "low")):
+        verify(x, what)
+
+
+def test_views_of_packed_projections(context):
+    """Three packed requests, q, k and v in one projection, out in [token][head][channel]; nothing beside the rows is touched."""
+    d, G, hk = 128, 4, 2
+    fin, gen = context("bf16", d, G), torch.Generator().manual_seed(5)
+    lens = [1, 50, 37]
+    x = randn(gen, sum(lens) + 1, (G * hk + 2 * hk), d)
+    x[-1] = math.nan
+    out = torch.full((sum(lens) + 1, G * hk, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    pbs, at = [], 0
+    for n in lens:
+        for g in range(hk):
+            pbs.append(dict(q=x[at:at + n, g * G:(g + 1) * G], k_chunk=x[at:at + n, G * hk + g], v_chunk=x[at:at + n, G * hk + hk + g],
+                            out=out[at:at + n, g * G:(g + 1) * G], causal=True))
+        at += n
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for i, pb in enumerate(pbs):
+        R.check_attention(pb["out"], None, pb["q"], pb["k_chunk"], pb["v_chunk"], True, f"packed {i}")
+    assert bool((out[-1] == 3).all())
+
+
+def test_rows_in_any_layout(context):
+    """Query rows and outputs by head first, candidates with room between their rows, a broadcast query."""
+    d, G = 64, 3
+    fin, gen = context("f32", d, G), torch.Generator().manual_seed(6)
+    q = randn(gen, G, 9, d + 4, dtype=torch.float32)
+    out = torch.zeros(G, 9, d + 12, device="cuda")
+    kv = randn(gen, 40, 2, 2 * d, dtype=torch.float32)
+    pbs = [dict(q=q[..., :d].transpose(0, 1), out=out[..., :d].transpose(0, 1), k_cache=kv[:31, 0, :d], v_cache=kv[:31, 1, :d], k_chunk=kv[31:, 0, d:],
+                v_chunk=kv[31:, 1, d:], causal=True),
+           dict(q=q[:1, :1, :d].expand(G, 4, d).transpose(0, 1), out=torch.zeros(4, G, d, device="cuda"), k_cache=kv[:7, 0, :d],
+                v_cache=kv[:7, 1, :d], causal=False)]
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for i, pb in enumerate(pbs):
+        k = [pb[n] for n in ("k_cache", "k_chunk") if n in pb]
+        v = [pb[n] for n in ("v_cache", "v_chunk") if n in pb]
+        R.check_attention(pb["out"], None, pb["q"], torch.cat(k), torch.cat(v), pb["causal"], f"layout {i}")
+    assert bool((out[..., d:] == 0).all())
+
+
+@pytest.mark.parametrize("live", [-3, 0, 1, 39, 40, 41, 1000])
+def test_chunk_length_from_the_device(context, live):
+    fin, gen = context("bf16", 128, 4), torch.Generator().manual_seed(7)
+    pbs = [problem(gen, "bf16", 128, 4, n, c, 40) for n, c in ((1, 70), (3, 0))]
+    there = min(40, max(0, live))
+    for pb in pbs:
+        pb["k_chunk"][there:] = math.nan  # not there yet
+        pb["v_chunk"][there:] = math.nan
+        pb["m_live"] = torch.tensor([live], dtype=torch.int32, device="cuda")
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for pb in pbs:
+        verify(pb, f"live={live}", m=there)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_further_apart_than_32_bits(context, dtype):
+    """A cache whose rows are spread over more than 4 GiB (2^32 bytes), and queries as well."""
+    fin, gen = context(dtype, 128, 2), torch.Generator().manual_seed(8)
+    dt, far = DT[dtype], 1 << 17
+    c = (1 << 32) // (far * dt.itemsize) + 70
+    big = torch.zeros(c, far, dtype=dt, device="cuda")
+    big[:, :256] = randn(gen, c, 256, dtype=dt)
+    q = randn(gen, 1, 2, 128, dtype=dt)
+    out, lse = torch.zeros(1, 2, 128, dtype=dt, device="cuda"), torch.zeros(2, device="cuda")
+    rows = torch.zeros(c, 2, 128, dtype=dt, device="cuda")
+    batch = [dict(q=q, k_cache=big[:, :128], v_cache=big[:, 128:256], out=out, lse=lse, causal=True),
+             dict(q=big[:, 512:768].view(c, 2, 128), k_chunk=big[:5, :128], v_chunk=big[:5, 128:256], out=rows, causal=False)]
+    fin.attend(F.AttentionBatch(batch))
+    torch.cuda.synchronize()
+    R.check_attention(out, lse, q, big[:, :128], big[:, 128:256], True, "far candidates")
+    # (queries of zeros: every row is the mean of the five values)
+    R.check_attention(rows[-40:], None, batch[1]["q"][-40:], big[:5, :128], big[:5, 128:256], False, "far queries")
+
+
+def test_same_bits_again_and_from_another_stream(context):
+    fin, gen = context("bf16", 128, 4), torch.Generator().manual_seed(9)
+    pbs = [problem(gen, "bf16", 128, 4, n, c, m) for n, c, m in ((1, 3000, 10), (200, 100, 200), (1, 90, 1))]
+    batch = F.AttentionBatch(pbs)
+    fin.attend(batch)
+    torch.cuda.synchronize()
+    first = [pb["out"].clone() for pb in pbs]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        for pb in pbs:
+            pb["out"].fill_(5)
+        fin.attend(batch)
+    s.synchronize()
+    for a, pb in zip(first, pbs):
+        assert torch.equal(a, pb["out"])
+    fin.attend(batch, stream=s.cuda_stream)
+    s.synchronize()
+    for a, pb in zip(first, pbs):
+        assert torch.equal(a, pb["out"])
+
+
+def test_two_captured_steps_that_share_a_workspace(context):
+    """Graphs on one workspace, replayed in turn with eager calls between, while one chunk grows."""
+    fin, gen = context("bf16", 128, 4), torch.Generator().manual_seed(10)
+    live = torch.tensor([1], dtype=torch.int32, device="cuda")
+    one = [problem(gen, "bf16", 128, 4, 1, 2000, 64) for _ in range(3)]
+    for pb in one:
+        pb["m_live"] = live
+    two = [problem(gen, "bf16", 128, 4, 30, 400, 30)]
+    b1, b2 = F.AttentionBatch(one), F.AttentionBatch(two)
+    fin.reserve_attend(b1), fin.reserve_attend(b2)
+    s = torch.cuda.Stream()
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1, stream=s):
+        fin.attend(b1)
+        live.add_(1)
+    with torch.cuda.graph(g2, stream=s):
+        fin.attend(b2)
+    live.fill_(1)
+    for step in range(1, 6):
+        for pb in one + two:
+            pb["out"].fill_(9)
+        g1.replay()
+        g2.replay()
+        torch.cuda.synchronize()
+        for pb in one:
+            verify(pb, f"replay {step}", m=step)
+        verify(two[0], f"replay {step} of the other")
+        fin.attend(b2)  # eager, on the same workspace
+        torch.cuda.synchronize()
+        verify(two[0], f"eager {step}")
+
+
+def test_no_rows_no_problems(context):
+    fin = context("bf16", 128, 4)
+    fin.attend(F.AttentionBatch([]))
+    x = torch.zeros(0, 4, 128, dtype=torch.bfloat16, device="cuda")
+    k = torch.ones(5, 128, dtype=torch.bfloat16, device="cuda")
+    fin.attend(F.AttentionBatch([dict(q=x, out=x.clone(), k_cache=k, v_cache=k)]))
+    torch.cuda.synchronize()
+
+
+def test_refusals_of_the_binding(context):
+    fin = context("bf16", 128, 4)
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    good = dict(q=z(2, 4, 128), out=z(2, 4, 128), k_cache=z(9, 128), v_cache=z(9, 128))
+    fin.attend(F.AttentionBatch([good]))
+    for bad in (dict(out=z(2, 4, 64)), dict(k_cache=z(8, 128)), dict(v_cache=None), dict(k_cache=z(9, 128, dtype=torch.float32)), dict(lse=z(7, dtype=torch.float32)),
+                dict(lse=z(8)), dict(m_live=z(1)), dict(q=z(2, 128, 4).transpose(1, 2)), dict(k_scale=z(1, dtype=torch.uint8)),
+                dict(k_scale=z(1, dtype=torch.uint8), v_scale=z(1, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            F.AttentionBatch([{**good, **bad}])
+    with pytest.raises(ValueError):  # another context's batch
+        fin.attend(F.AttentionBatch([dict(q=z(2, 2, 128), out=z(2, 2, 128), k_cache=z(9, 128), v_cache=z(9, 128))]))
+    e = dict(q=z(1, 4, 128), out=z(1, 4, 128), k_cache=z(129, 128, dtype=torch.uint8), v_cache=z(129, 128, dtype=torch.uint8),
+             k_scale=z(2, dtype=torch.uint8), v_scale=z(2, dtype=torch.uint8))
+    with pytest.raises(ValueError):  # 129 rows are three blocks of 64
+        fin.attend(F.AttentionBatch([e]))
+    with pytest.raises(F.FinchError) as err:
+        fin.attend(F.AttentionBatch([{**good, "out": good["q"]}]))
+    assert err.value.status == F.FINCH_ERR_INVALID_ARG
+    big = problem(torch.Generator().manual_seed(1), "bf16", 128, 4, 1, 9000, 1)
+    batch = F.AttentionBatch([big])
+    need = F.finch_attend_workspace_size(fin.ctx, batch.host, 1)
+    assert need > 0
+    with pytest.raises(F.FinchError) as err:
+        F.finch_attend(fin.ctx, batch.host, batch.dev_ptr, 1, fin.ws.data_ptr(), need - 1)
+    assert err.value.status == F.FINCH_ERR_WORKSPACE

@@ -1,0 +1,238 @@
+"""finch_rotate and finch_quantize against the definition in 64 bits, and a layer's whole way: rotate, score, select, compact,
+quantize, attend."""
+import math
+
+import pytest
+import torch
+
+import paper_2408_00167_amd as F
+from tests import layer_reference as R
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def make(dtype, d, G):
+    return F.Finch(F.FINCH_BF16 if dtype == "bf16" else F.FINCH_F32, d, G)
+
+
+def rotary(gen, dt, d, pairing, dims, norm, scaling=F.FINCH_SCALING_NONE, base=10000.0):
+    freq, gain = F.finch_rope_frequencies(dims, base, scaling, 8.0, 1.0, 4.0, 8192)
+    w = [(1 + 0.3 * torch.randn(d, generator=gen)).to(dt).cuda() if norm else None for _ in range(2)]
+    how = F.Rotary(pairing, dims, torch.tensor(freq, dtype=torch.float64, device="cuda"), gain, w[0], w[1], 1e-5)
+    return how, freq, gain, w
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("pairing", [F.FINCH_ROPE_HALF, F.FINCH_ROPE_INTERLEAVED])
+@pytest.mark.parametrize("norm", [False, True])
+def test_rotate_ragged_packed_and_paged(dtype, d, pairing, norm):
+    dt, G, hk = DT[dtype], 3, 2
+    gen = torch.Generator().manual_seed(1)
+    fin = make(dtype, d, G)
+    for dims in sorted({d, d // 2, 48}):
+        how, freq, gain, w = rotary(gen, dt, d, pairing, dims, norm, F.FINCH_SCALING_RAMP if dims == d else F.FINCH_SCALING_BANDED)
+        lens = [1, 0, 5, 33, 4]
+        total = sum(lens)
+        x = torch.randn(total, (G + 2) * hk, d, generator=gen).to(dt).cuda()
+        pos = torch.randint(-5, 200000, (total,), generator=gen, dtype=torch.int32).cuda()
+        # pages in any order, one token of padding, one slot past the end
+        room = 64
+        slot = torch.randperm(room, generator=gen)[:total].int().cuda()
+        slot[3], slot[7] = -1, room
+        q_out = torch.full((G * hk, total + 1, d), 3.0, dtype=dt, device="cuda")
+        k_out, v_out = (torch.full((room + 2, hk, d), 5.0, dtype=dt, device="cuda") for _ in range(2))
+        reqs, at = [], 0
+        for n in lens:
+            s = slice(at, at + n)
+            reqs.append(dict(q=x[s, :G * hk], k=x[s, G * hk:G * hk + hk], v=x[s, G * hk + hk:], pos=pos[s], slot=slot[s],
+                             q_out=q_out[:, s].transpose(0, 1), k_out=k_out[1:-1], v_out=v_out[1:-1]))
+            at += n
+        fin.rotate(F.RowsBatch(reqs), how)
+        torch.cuda.synchronize()
+        what = f"{dtype} d={d} pairing={pairing} norm={norm} dims={dims}"
+        p = pos.tolist()
+        R.check_rotated(q_out[:, :total].transpose(0, 1), x[:, :G * hk], p, pairing, dims, freq, gain, w[0], 1e-5, what + " q")
+        assert bool((q_out[:, total] == 3).all())
+        ok = [i for i in range(total) if 0 <= slot[i] < room]
+        rows = slot[ok].long() + 1
+        R.check_rotated(k_out[rows], x[ok, G * hk:G * hk + hk], [p[i] for i in ok], pairing, dims, freq, gain, w[1], 1e-5, what + " k")
+        assert torch.equal(v_out[rows], x[ok, G * hk + hk:])
+        rest = torch.ones(room + 2, dtype=torch.bool)
+        rest[rows.cpu()] = False
+        assert bool((k_out[rest] == 5).all()) and bool((v_out[rest] == 5).all()), what + ": rows nobody wrote"
+    fin.close()
+
+
+def test_rotate_parts_alone_in_place_and_off():
+    fin, gen = make("bf16", 128, 2), torch.Generator().manual_seed(2)
+    how, freq, gain, _ = rotary(gen, torch.bfloat16, 128, F.FINCH_ROPE_HALF, 128, False)
+    x = torch.randn(9, 8, 128, generator=gen).to(torch.bfloat16).cuda()  # 4 query heads, 2 + 2
+    q, k, v = x[:, :4].clone(), x[:, 4:6].clone(), x[:, 6:].clone()
+    y = x.clone()
+    fin.rotate(F.RowsBatch([dict(q=y[:, :4], q_out=y[:, :4], k=y[:, 4:6], k_out=y[:, 4:6], pos0=100)]), how)  # in place
+    only = torch.zeros_like(q)
+    fin.rotate(F.RowsBatch([dict(q=q, q_out=only, kv_heads=2, pos0=100)]), how)
+    vo = torch.zeros_like(v)
+    fin.rotate(F.RowsBatch([dict(v=v, v_out=vo)]), F.Rotary(F.FINCH_ROPE_OFF))
+    same = torch.zeros_like(k)
+    fin.rotate(F.RowsBatch([dict(k=k, k_out=same)]), F.Rotary(F.FINCH_ROPE_OFF))
+    still = torch.zeros_like(k)
+    fin.rotate(F.RowsBatch([dict(k=k[:1], k_out=still[:1], pos0=0)]), how)  # position 0 turns nothing
+    torch.cuda.synchronize()
+    p = list(range(100, 109))
+    R.check_rotated(y[:, :4], q, p, 1, 128, freq, gain, None, 0, "q in place")
+    R.check_rotated(y[:, 4:6], k, p, 1, 128, freq, gain, None, 0, "k in place")
+    assert torch.equal(only, y[:, :4]) and torch.equal(y[:, 6:], v) and torch.equal(vo, v) and torch.equal(same, k)
+    assert torch.equal(still[:1], k[:1])
+    fin.close()
+
+
+def test_rotate_norm_of_zeros_and_extremes():
+    fin = make("f32", 64, 1)
+    w = torch.ones(64, device="cuda")
+    x = torch.zeros(3, 1, 64, device="cuda")
+    x[1] = 1e-15
+    x[2, 0, 5] = 1e15
+    out = torch.full_like(x, 9)
+    fin.rotate(F.RowsBatch([dict(k=x, k_out=out)]), F.Rotary(F.FINCH_ROPE_OFF, k_norm=w, eps=1e-6))
+    torch.cuda.synchronize()
+    R.check_rotated(out, x, [0, 0, 0], 0, 0, [], 1.0, w, 1e-6, "norm")
+    fin.close()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+def test_quantize_bits(dtype, d, block):
+    fin, gen = make(dtype, d, 1), torch.Generator().manual_seed(3)
+    fin.set_scale_block(block)
+    pbs = []
+    for n in (0, 1, 15, 16, 17, 63, 64, 65, 128, 129, 500):
+        pb = {}
+        for name in ("k", "v"):
+            size = torch.exp(4 * torch.randn(n, 1, generator=gen)) * torch.exp(torch.randn(1, d, generator=gen))
+            x = torch.randn(n, d, generator=gen) * size
+            if n > 40:
+                x[16:32] = 0                              # a block of zeros
+                x[32] = torch.tensor([448.0, 1.0625, -1.1875, 2.0 ** -10] * (d // 4))  # ties
+                x[33:36] *= 2.0 ** -118                   # far below the rest
+            pb[name] = x.to(DT[dtype]).cuda()
+            pb[name + "_all"] = torch.full((n + 2, d), 0x55, dtype=torch.uint8, device="cuda")
+            pb[name + "_out"] = pb[name + "_all"][1:n + 1]
+            pb[name + "_scales"] = torch.full((-(-n // block) + 1,), 77, dtype=torch.uint8, device="cuda")
+            pb[name + "_scale"] = pb[name + "_scales"][:max(1, -(-n // block))]
+        pbs.append(pb)
+    tiny = {name: torch.full((20, d), 2.0 ** -126, dtype=DT[dtype], device="cuda") for name in ("k", "v")}
+    for name in ("k", "v"):
+        tiny[name + "_out"], tiny[name + "_scale"] = torch.ones(20, d, dtype=torch.uint8, device="cuda"), torch.zeros(2, dtype=torch.uint8, device="cuda")
+    fin.quantize(F.QuantizeBatch(pbs + [tiny]))
+    torch.cuda.synchronize()
+    for pb in pbs + [tiny]:
+        n = pb["k"].shape[0]
+        for name in ("k", "v"):
+            want, exps = R.quantized(pb[name], block)
+            assert pb[name + "_scale"][:-(-n // block)].tolist() == [e + 127 for e in exps], f"{dtype} {d} {block} {n} {name}"
+            assert torch.equal(R.e4m3_values(pb[name + "_out"]), want), f"{dtype} {d} {block} {n} {name}"
+            if name + "_all" in pb:
+                assert bool((pb[name + "_all"][0] == 0x55).all()) and bool((pb[name + "_all"][-1] == 0x55).all())
+                assert pb[name + "_scales"][-1] == 77
+    fin.close()
+
+
+def test_quantize_strided_rows():
+    fin, gen = make("bf16", 128, 1), torch.Generator().manual_seed(4)
+    x = torch.randn(70, 2, 3, 128, generator=gen).to(torch.bfloat16).cuda()
+    y = torch.full((70, 2, 144), 7, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(2, 2, dtype=torch.uint8, device="cuda")
+    fin.quantize(F.QuantizeBatch([dict(k=x[:, 0, 1], v=x[:, 1, 2], k_out=y[:, 0, :128], v_out=y[:, 1, :128], k_scale=s[0], v_scale=s[1])]))
+    torch.cuda.synchronize()
+    for i, t in enumerate((x[:, 0, 1], x[:, 1, 2])):
+        want, exps = R.quantized(t, 64)
+        assert torch.equal(R.e4m3_values(y[:, i, :128].contiguous()), want) and s[i].tolist() == [e + 127 for e in exps]
+    assert bool((y[..., 128:] == 7).all())
+    fin.close()
+
+
+def test_refusals_of_the_binding():
+    fin = make("bf16", 128, 2)
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    good = dict(q=z(3, 4, 128), k=z(3, 2, 128), v=z(3, 2, 128), q_out=z(3, 4, 128), k_out=z(3, 2, 128), v_out=z(3, 2, 128))
+    fin.rotate(F.RowsBatch([good]), F.Rotary(F.FINCH_ROPE_OFF))
+    for bad in (dict(q=z(2, 4, 128)), dict(k=z(3, 3, 128)), dict(q_out=z(4, 4, 128)), dict(k_out=z(3, 2, 64)), dict(v=z(3, 2, 128, dtype=torch.float32)),
+                dict(pos=z(3, dtype=torch.int64)), dict(slot=z(2, dtype=torch.int32)), dict(q=z(3, 5, 128), q_out=z(3, 5, 128))):
+        with pytest.raises(ValueError):
+            F.RowsBatch([{**good, **bad}])
+    with pytest.raises(ValueError):
+        F.Rotary(F.FINCH_ROPE_HALF, 128, z(32, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        fin.rotate(F.RowsBatch([good]), F.Rotary(F.FINCH_ROPE_OFF, q_norm=z(64)))
+    with pytest.raises(ValueError):
+        fin.rotate(F.RowsBatch([{**good, "q": z(3, 2, 128), "q_out": z(3, 2, 128)}]), F.Rotary(F.FINCH_ROPE_OFF))
+    s = z(2, dtype=torch.uint8)
+    q8 = dict(k=z(200, 128), v=z(200, 128), k_out=z(200, 128, dtype=torch.uint8), v_out=z(200, 128, dtype=torch.uint8), k_scale=s, v_scale=s.clone())
+    with pytest.raises(ValueError):  # 200 rows are four blocks of 64
+        fin.quantize(F.QuantizeBatch([q8]))
+    with pytest.raises(ValueError):
+        F.QuantizeBatch([{**q8, "v": z(199, 128)}])
+    fin.close()
+
+
+def test_a_layer_from_projections_to_generated_tokens():
+    """A document chunk and a prompt go through a layer: rotated and placed, attended to, scored and compacted; the kept rows go to
+    8 bits, and generated tokens attend over them, in a captured step that is replayed while the tail grows."""
+    d, G, hk, m, nq, keep, steps, room = 128, 4, 2, 300, 24, 96, 6, 16
+    hq = G * hk
+    fin, gen = make("bf16", d, G), torch.Generator().manual_seed(5)
+    how, freq, gain, _ = rotary(gen, torch.bfloat16, d, F.FINCH_ROPE_HALF, d, False, base=500000.0)
+    n = m + nq
+    x = torch.randn(n, hq + 2 * hk, d, generator=gen).to(torch.bfloat16).cuda()
+    q = torch.zeros(hq, n, d, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros(hk, n, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    fin.rotate(F.RowsBatch([dict(q=x[:, :hq], k=x[:, hq:hq + hk], v=x[:, hq + hk:], q_out=q.transpose(0, 1), k_out=k.transpose(0, 1),
+                                 v_out=v.transpose(0, 1))]), how)
+    out = torch.zeros(n, hq, d, dtype=torch.bfloat16, device="cuda")
+    fin.attend(F.AttentionBatch([dict(q=q[g * G:(g + 1) * G].transpose(0, 1), out=out[:, g * G:(g + 1) * G], k_chunk=k[g], v_chunk=v[g])
+                                 for g in range(hk)]))
+    # the prompt's rows choose among the chunk's
+    prompt = [q[g * G:(g + 1) * G, m:].reshape(G * nq, d).contiguous() for g in range(hk)]
+    kept = [dict(q=prompt[g], k_chunk=k[g, :m], v_chunk=v[g, :m], k_out=torch.zeros(keep, d, dtype=torch.bfloat16, device="cuda"),
+                 v_out=torch.zeros(keep, d, dtype=torch.bfloat16, device="cuda"), scores=torch.zeros(m, device="cuda"),
+                 idx=torch.zeros(keep, dtype=torch.int32, device="cuda"), n_que=nq, c=0, m=m, r=keep) for g in range(hk)]
+    fin.step(F.Batch(kept))
+    small = [dict(k=c["k_out"], v=c["v_out"], k_out=torch.zeros(keep, d, dtype=torch.uint8, device="cuda"),
+                  v_out=torch.zeros(keep, d, dtype=torch.uint8, device="cuda"), k_scale=torch.zeros(2, dtype=torch.uint8, device="cuda"),
+                  v_scale=torch.zeros(2, dtype=torch.uint8, device="cuda")) for c in kept]
+    fin.quantize(F.QuantizeBatch(small))
+    torch.cuda.synchronize()
+    for g in range(hk):
+        R.check_rotated(k[g][:, None], x[:, hq + g:hq + g + 1], range(n), 1, d, freq, gain, None, 0, f"keys of head {g}")
+        R.check_attention(out[:, g * G:(g + 1) * G], None, q[g * G:(g + 1) * G].transpose(0, 1), k[g], v[g], True, f"chunk, head {g}")
+        want, exps = R.quantized(kept[g]["k_out"], 64)
+        assert torch.equal(R.e4m3_values(small[g]["k_out"]), want)
+    # generated tokens: their projections arrive one by one, K and V are appended to a tail of 16-bit rows
+    new = torch.randn(steps, 1, hq + 2 * hk, d, generator=gen).to(torch.bfloat16).cuda()
+    tail = torch.full((2, hk, room, d), math.nan, dtype=torch.bfloat16, device="cuda")
+    now, tq, tout = new[0].clone(), torch.zeros(1, hq, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, hq, d, dtype=torch.bfloat16, device="cuda")
+    pos, slot, live = (torch.tensor([t], dtype=torch.int32, device="cuda") for t in (n, 0, 1))
+    rows = F.RowsBatch([dict(q=now[:, :hq], k=now[:, hq:hq + hk], v=now[:, hq + hk:], q_out=tq, k_out=tail[0].transpose(0, 1),
+                             v_out=tail[1].transpose(0, 1), pos=pos, slot=slot)])
+    step = F.AttentionBatch([dict(q=tq[:, g * G:(g + 1) * G], out=tout[:, g * G:(g + 1) * G], k_cache=small[g]["k_out"], v_cache=small[g]["v_out"],
+                                  k_scale=small[g]["k_scale"], v_scale=small[g]["v_scale"], k_chunk=tail[0, g], v_chunk=tail[1, g], m_live=live)
+                             for g in range(hk)])
+    fin.reserve_attend(step)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        fin.rotate(rows, how)
+        fin.attend(step)
+        for t in (pos, slot, live):
+            t.add_(1)
+    for i in range(steps):
+        now.copy_(new[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        for g in range(hk):
+            R.check_rotated(tail[0, g, i][None, None], new[i][:, hq + g:hq + g + 1], [n + i], 1, d, freq, gain, None, 0, f"token {i}: key")
+            kc, vc = (R.dequantized(small[g][name + "_out"], small[g][name + "_scale"], 64) for name in ("k", "v"))
+            R.check_attention(tout[:, g * G:(g + 1) * G], None, tq[:, g * G:(g + 1) * G], torch.cat([kc, R.host(tail[0, g, :i + 1])]),
+                              torch.cat([vc, R.host(tail[1, g, :i + 1])]), True, f"token {i}, head {g}")
+    fin.close()
