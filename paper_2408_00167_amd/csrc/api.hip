@@ -913,6 +913,7 @@ finch_status finch_create(const finch_config* cfg, finch_ctx** out) {
   if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = finch::set_max_lds_cluster(ctx->max_lds);
   if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = make_meet(&ctx->meet, a.stream);
   if (e == hipSuccess) e = finch::set_max_lds_select(ctx->max_lds);
+  if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = finch::set_max_lds_attend();
   // the re-positioning kernel also has a little static LDS
   if (e == hipSuccess) e = finch::set_max_lds_reposition(ctx->max_lds - 1024);
   if (e != hipSuccess) {

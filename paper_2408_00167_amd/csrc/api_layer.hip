@@ -1,6 +1,7 @@
 // Entry points around the compression in a model's layer: finch_rotate, finch_rope_frequencies,
 // finch_quantize, finch_attend.  Argument checks, launch sizing, launches; no allocation and no
 // synchronisation.
+#include <algorithm>
 #include <cmath>
 
 #include "attend.h"
@@ -64,12 +65,18 @@ bool between_rows(const void* a, const void* b, int64_t n, int64_t row, int64_t 
 constexpr int32_t kMostRows = 1 << 24;
 constexpr int32_t kMostHeads = 1 << 12;
 
-// How one batch of finch_attend is launched.
+// How one batch of finch_attend is launched: problems of few rows and of many by kernels of their own.
 struct AttendPlan {
+  struct Part {
+    int tile_rows, tile_keys;
+    int rows_lo = 0, rows_hi = 0, row_tiles = 0;  // (no row tiles: nothing to launch)
+    int64_t splits = 1, span = 1;
+    size_t off_o = 0, off_ml = 0;
+    // of its problems: tiles of rows, tiles of keys that these see, most tiles of keys
+    int64_t tiles = 0, work = 0, keys_max = 0;
+  } few, many;
   bool eight = false;
-  int tile_rows = 0, tile_keys = 0;
-  int row_tiles = 0, splits = 1, span = 1;
-  size_t off_ml = 0, bytes = 0;
+  size_t bytes = 0;
 };
 
 finch_status check_attention(const finch_ctx* ctx, const finch_attention& a) {
@@ -99,46 +106,64 @@ finch_status check_attention(const finch_ctx* ctx, const finch_attention& a) {
   return FINCH_OK;
 }
 
-// Splits.  Every tile of rows is a workgroup's; where these are too few for the chip, the keys are dealt out to
-// several: `span` tiles each, so that all of them together are about two rounds of workgroups.
+// Most stacked rows that go the way of few rows.
+constexpr int kFewRows = 64;
+
+void count(AttendPlan::Part& pt, const finch_attention& a, int64_t rows) {
+  const int64_t tiles = (rows + pt.tile_rows - 1) / pt.tile_rows, cache = (a.c + pt.tile_keys - 1) / pt.tile_keys;
+  const int64_t keys = cache + (a.m + pt.tile_keys - 1) / pt.tile_keys;
+  if (tiles > pt.row_tiles) pt.row_tiles = static_cast<int>(tiles);
+  if (keys > pt.keys_max) pt.keys_max = keys;
+  pt.tiles += tiles;
+  // (causal rows of the chunk itself see half of themselves on average)
+  const int64_t own = a.causal ? std::min(a.n_que, a.m) / 2 / pt.tile_keys : 0;
+  pt.work += tiles * (keys - own);
+}
+
+// Splits: where tiles of rows are too few for the chip, the keys each sees are dealt out to several workgroups of `span` tiles at
+// least, so that there are about `groups` workgroups.
+finch_status split(AttendPlan::Part& pt, int64_t n, int64_t groups, int64_t span_min, int64_t enough, int head_dim, size_t& off) {
+  const int64_t tiles = n * pt.row_tiles, part = int64_t{pt.tile_rows} * (head_dim + 2) * 4;
+  if (tiles == 0) return FINCH_OK;
+  pt.span = std::max((pt.work + groups - 1) / groups, span_min);
+  if (pt.tiles >= enough) pt.span = std::max<int64_t>(pt.keys_max, 1);
+  // (partial results of at most 64 MiB and 2^15 tiles of rows)
+  const int64_t most = std::max<int64_t>(1, std::min((int64_t{64} << 20) / part, int64_t{1} << 15) / tiles);
+  pt.splits = std::max<int64_t>(1, (pt.keys_max + pt.span - 1) / pt.span);
+  if (pt.splits > most) {
+    pt.splits = most;
+    pt.span = (pt.keys_max + most - 1) / most;
+  }
+  if (tiles * pt.splits >= (int64_t{1} << 22)) return FINCH_ERR_CAPACITY;
+  if (pt.splits > 1) {
+    pt.off_o = off;
+    off = align_up(off + static_cast<size_t>(tiles * pt.splits) * pt.tile_rows * head_dim * 4, 256);
+    pt.off_ml = off;
+    off = align_up(off + static_cast<size_t>(tiles * pt.splits) * pt.tile_rows * 8, 256);
+  }
+  return FINCH_OK;
+}
+
 finch_status plan_attention(const finch_ctx* ctx, const finch_attention* hd, int32_t n, AttendPlan& pl) {
   const bool bf16 = ctx->cfg.dtype == FINCH_BF16;
   const int G = ctx->cfg.group_size, cu = ctx->n_cu > 0 ? ctx->n_cu : 256;
-  pl.tile_rows = bf16 ? finch::kRowsTile : finch::kF32Tile;
-  pl.tile_keys = bf16 ? finch::kRowsKeys : finch::kF32Keys;
-  int64_t rows_max = 0, work = 0, tiles_max = 0;
+  pl.few.tile_rows = bf16 ? finch::kRowsTile : finch::kF32Tile;
+  pl.few.tile_keys = bf16 ? finch::kRowsKeys : finch::kF32Keys;
+  pl.few.rows_hi = bf16 ? kFewRows : INT32_MAX;
+  pl.many.tile_rows = finch::kTilesRows;
+  pl.many.tile_keys = finch::kTilesKeys;
+  pl.many.rows_lo = kFewRows + 1;
+  pl.many.rows_hi = INT32_MAX;
   for (int32_t i = 0; i < n; ++i) {
     const finch_status st = check_attention(ctx, hd[i]);
     if (st != FINCH_OK) return st;
     if (hd[i].k_scale) pl.eight = true;
     const int64_t rows = int64_t{hd[i].n_que} * G;
-    const int64_t tiles = (hd[i].c + pl.tile_keys - 1) / pl.tile_keys + (hd[i].m + pl.tile_keys - 1) / pl.tile_keys;
-    if (rows > rows_max) rows_max = rows;
-    if (rows > 0 && tiles > tiles_max) tiles_max = tiles;
-    work += (rows + pl.tile_rows - 1) / pl.tile_rows * tiles;
+    if (rows > 0) count(rows <= pl.few.rows_hi ? pl.few : pl.many, hd[i], rows);
   }
-  pl.row_tiles = static_cast<int>((rows_max + pl.tile_rows - 1) / pl.tile_rows);
-  const int64_t groups = 4 * cu;
-  int64_t span = (work + groups - 1) / groups;
-  if (span < 4) span = 4;  // a tile per wave
-  // (partial results of at most 64 MiB and 2^15 tiles of rows)
-  const int64_t tiles = int64_t{n} * pl.row_tiles, part = int64_t{pl.tile_rows} * (ctx->cfg.head_dim + 2) * 4;
-  int64_t most = tiles > 0 ? std::min((int64_t{64} << 20) / part, int64_t{1} << 15) / tiles : 1;
-  if (most < 1) most = 1;
-  int64_t splits = (tiles_max + span - 1) / span;
-  if (splits > most) {
-    splits = most;
-    span = (tiles_max + splits - 1) / splits;
-  }
-  if (splits < 1) splits = 1;
-  pl.splits = static_cast<int>(splits);
-  pl.span = static_cast<int>(span);
-  if (tiles * splits >= (int64_t{1} << 23)) return FINCH_ERR_CAPACITY;
-  if (splits > 1) {
-    pl.off_ml = align_up(static_cast<size_t>(tiles * splits) * pl.tile_rows * ctx->cfg.head_dim * 4, 256);
-    pl.bytes = align_up(pl.off_ml + static_cast<size_t>(tiles * splits) * pl.tile_rows * 8, 256);
-  }
-  return FINCH_OK;
+  finch_status st = split(pl.few, n, 4 * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
+  if (st == FINCH_OK) st = split(pl.many, n, 2 * cu, 8, cu, ctx->cfg.head_dim, pl.bytes);
+  return st;
 }
 
 finch_status check_rotation(const finch_ctx* ctx, const finch_rotary* how, const finch_rows* hd, int32_t n, int32_t& n_max) {
@@ -284,24 +309,35 @@ finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, cons
   AttendPlan pl;
   if ((st = plan_attention(ctx, host_desc, n, pl)) != FINCH_OK) return st;
   if (pl.bytes > 0 && (!ws || !aligned(ws, 256) || ws_bytes < pl.bytes)) return FINCH_ERR_WORKSPACE;
-  if (n == 0 || pl.row_tiles == 0) return FINCH_OK;
-  AttendParams p;
-  p.descs = dev_desc;
-  p.n = n;
-  p.group = ctx->cfg.group_size;
-  p.row_tiles = pl.row_tiles;
-  p.splits = pl.splits;
-  p.span = pl.span;
-  p.block_shift = __builtin_ctz(static_cast<unsigned>(ctx->scale_block));
-  p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(ctx->cfg.head_dim)));
-  p.part = static_cast<float*>(ws);
-  p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + pl.off_ml);
+  if (pl.few.row_tiles == 0 && pl.many.row_tiles == 0) return FINCH_OK;
   const OnDevice on(ctx);
   if (on.e != hipSuccess) return done(ctx, on.e);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = ctx->cfg.dtype == FINCH_BF16;
-  hipError_t e = bf16 ? finch::launch_attend_rows(ctx->cfg.head_dim, pl.eight, p, s) : finch::launch_attend_rows_f32(ctx->cfg.head_dim, p, s);
-  if (e == hipSuccess && pl.splits > 1) e = finch::launch_attend_join(ctx->cfg.head_dim, bf16, pl.tile_rows, pl.tile_keys, p, s);
+  const int d = ctx->cfg.head_dim;
+  hipError_t e = hipSuccess;
+  for (const AttendPlan::Part* pt : {&pl.many, &pl.few}) {
+    if (pt->row_tiles == 0) continue;
+    AttendParams p;
+    p.descs = dev_desc;
+    p.n = n;
+    p.group = ctx->cfg.group_size;
+    p.rows_lo = pt->rows_lo;
+    p.rows_hi = pt->rows_hi;
+    p.row_tiles = pt->row_tiles;
+    p.splits = static_cast<int32_t>(pt->splits);
+    p.span = static_cast<int32_t>(pt->span);
+    p.block_shift = __builtin_ctz(static_cast<unsigned>(ctx->scale_block));
+    p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(d)));
+    p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pt->off_o);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + pt->off_ml);
+    if (e == hipSuccess) {
+      e = pt == &pl.many ? finch::launch_attend_tiles(d, pl.eight, p, s)
+          : bf16         ? finch::launch_attend_rows(d, pl.eight, p, s)
+                         : finch::launch_attend_rows_f32(d, p, s);
+    }
+    if (e == hipSuccess && pt->splits > 1) e = finch::launch_attend_join(d, bf16, pt->tile_rows, pt->tile_keys, p, s);
+  }
   return done(ctx, e);
 }
 

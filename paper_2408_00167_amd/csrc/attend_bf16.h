@@ -1,0 +1,100 @@
+// What the bf16 attention kernels share: where rows lie, e4m3 to bf16, the running softmax of a lane's row,
+// V^T out of LDS.
+#pragma once
+
+#include "attend_common.h"
+
+namespace finch {
+
+typedef __attribute__((address_space(3))) s16x4* lds_tr;
+
+// rows of K or V in memory
+struct Part {
+  const char* k;
+  const char* v;
+  long long row;  // bytes
+  int n;          // rows
+  const unsigned char* ks;
+  const unsigned char* vs;
+};
+
+// 8 e4m3 numbers times 2^(e - 127) as bf16: exact, one instruction for two.
+__device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi, unsigned e) {
+  const float f = __uint_as_float(e << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Which piece of row r takes the place of piece 0 in LDS: rows 0..7 (0..3 with 64 channels) differ by two pieces.
+template <int D>
+__device__ __forceinline__ int swap_of(int r) {
+  return 2 * (r & (D == 128 ? 7 : 3));
+}
+
+// The rows' state in a lane: reference (log2 domain), sum of the lane's weights, O^T.
+template <int D>
+struct Rows {
+  float ref = -kInf, sum = 0.f;
+  f32x16 o[D / 32];
+};
+
+// Logits of one row against NB blocks of 32 keys become weights: the maximum moves the reference if it is far above it,
+// the weights' sum goes to the lane's.
+template <int D, int NB>
+__device__ __forceinline__ void weigh(Rows<D>& st, f32x16* s, float scale) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+  mx = fmaxf(mx, other_half(mx)) * scale;
+  if (__any(mx > st.ref + kSlack)) {
+    const float ref = fmaxf(st.ref, mx);
+    const float f = st.ref == -kInf ? 0.f : fast_exp2(st.ref - ref);
+    st.ref = ref;
+    st.sum *= f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) st.o[db][v] *= f;
+  }
+  const float ref = st.ref == -kInf ? 0.f : st.ref;
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      s[kb][v] = fast_exp2(fmaf(s[kb][v], scale, -ref));
+      st.sum += s[kb][v];
+    }
+}
+
+// Where a lane reads V^T in LDS: keys 4h + (lane & 15) / 4 of a step of 16, columns of its 16-lane group.
+template <int D>
+__device__ __forceinline__ void v_offsets(int (&off)[D / 32], int lane) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    const int key = 4 * (lane >> 5) + ((lane & 15) >> 2), pc = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    off[db] = key * (2 * D) + (pc ^ swap_of<D>(key)) * 16 + 8 * (lane & 1);
+  }
+}
+
+// O^T += V^T P^T for NB blocks of 32 keys.
+template <int D, int NB>
+__device__ __forceinline__ void add_values(Rows<D>& st, const f32x16* s, const char* lds, const int (&off)[D / 32]) {
+#pragma unroll
+  for (int b = 0; b < 2 * NB; ++b) {
+    bf16x8 pf;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) pf[v] = static_cast<__bf16>(s[b >> 1][8 * (b & 1) + v]);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b) * (2 * D)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b + 8) * (2 * D)));
+      const s16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf, st.o[db], 0, 0, 0);
+    }
+  }
+}
+
+}  // namespace finch

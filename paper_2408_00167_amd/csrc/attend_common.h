@@ -24,6 +24,7 @@ struct AttendParams {
   const finch_attention* descs;
   int32_t n;            // problems
   int32_t group;        // G
+  int32_t rows_lo, rows_hi;  // problems with as many stacked rows are this launch's
   int32_t row_tiles;    // of the problem with the most rows
   int32_t splits;       // most workgroups on one tile of rows
   int32_t span;         // tiles of keys a split has at least (but the last)
@@ -36,6 +37,7 @@ struct AttendParams {
 // rows and keys of a tile
 constexpr int kRowsTile = 32, kRowsKeys = 32, kRowsWaves = 4;    // attend_rows
 constexpr int kF32Tile = 16, kF32Keys = 16, kF32Waves = 4;       // attend_rows_f32
+constexpr int kTilesRows = 256, kTilesKeys = 64, kTilesWaves = 8;  // attend_tiles
 
 __device__ __forceinline__ finch_attention load_attention(const finch_attention* p) {
   typedef const __attribute__((address_space(4))) unsigned long long* words;
@@ -60,6 +62,8 @@ struct Seen {
     if (d.m_live) m = min(m, max(0, uni(*as_global<int>(d.m_live))));
     R = d.n_que * group;
   }
+  // whether row r0 is this launch's
+  __device__ __forceinline__ bool has(const AttendParams& prm, int r0) const { return R >= prm.rows_lo && R <= prm.rows_hi && r0 < R; }
   // candidates that stacked row rr sees
   __device__ __forceinline__ int limit(int rr) const {
     const int all = d.c + m;

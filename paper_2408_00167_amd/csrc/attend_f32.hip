@@ -14,7 +14,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
   const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = rest % prm.row_tiles, split = rest / prm.row_tiles;
   const Seen pb(prm, p);
   const int r0 = rt * kF32Tile;
-  if (r0 >= pb.R) return;
+  if (!pb.has(prm, r0)) return;
   const Share sh(prm, pb, r0, kF32Tile, kF32Keys, split);
   if (split >= sh.active) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), row = lane & 15, part = lane >> 4;

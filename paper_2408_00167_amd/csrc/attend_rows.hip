@@ -15,22 +15,11 @@
 //
 // K of the next tile is under way while the softmax runs, V of the next tile during P V.
 #include "attend.h"
+#include "attend_bf16.h"
 
 namespace finch {
 
 namespace {
-
-typedef __attribute__((address_space(3))) s16x4* lds_tr;
-
-// rows of K or V in memory
-struct Part {
-  const char* k;
-  const char* v;
-  long long row;  // bytes
-  int n;          // rows
-  const unsigned char* ks;
-  const unsigned char* vs;
-};
 
 template <int D, bool E8>
 struct Tile {
@@ -69,20 +58,6 @@ __device__ __forceinline__ void load_v(Tile<D, E8>& t, const Part& a, int key0, 
   }
 }
 
-// 8 e4m3 numbers times 2^(e - 127) as bf16: exact, one instruction for two.
-__device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi, unsigned e) {
-  const float f = __uint_as_float(e << 23);
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// Which piece of row r takes the place of piece 0 in LDS: rows 0..7 (0..3 with 64 channels) differ by two pieces.
-template <int D>
-__device__ __forceinline__ int swap_of(int r) {
-  return 2 * (r & (D == 128 ? 7 : 3));
-}
-
 template <int D, bool E8>
 __device__ __forceinline__ void v_to_lds(const Tile<D, E8>& t, char* lds, int lane) {
   constexpr int kPer = D / (E8 ? 16 : 8);
@@ -99,13 +74,6 @@ __device__ __forceinline__ void v_to_lds(const Tile<D, E8>& t, char* lds, int la
   }
 }
 
-// The rows' state in a lane: reference (log2 domain), sum of the lane's weights, O^T.
-template <int D>
-struct Rows {
-  float ref = -kInf, sum = 0.f;
-  f32x16 o[D / 32];
-};
-
 // Tiles first, first + step, ... below last of one part (or, for bf16, of both one after the other).
 template <int D, bool E8>
 __device__ __forceinline__ void stream(Rows<D>& st, const bf16x8 (&q)[D / 16], const Part& cache, const Part& chunk, int cache_tiles,
@@ -115,13 +83,8 @@ __device__ __forceinline__ void stream(Rows<D>& st, const bf16x8 (&q)[D / 16], c
   Tile<D, E8> t;
   const auto part = [&](int i) -> Part { return i < cache_tiles ? cache : chunk; };
   const auto key0 = [&](int i) { return (i < cache_tiles ? i : i - cache_tiles) * kRowsKeys; };
-  // where a lane reads V^T: keys 4h + (lane & 15) / 4 of a step, columns of its 16-lane group
   int off[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db) {
-    const int key = 4 * h + ((lane & 15) >> 2), pc = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    off[db] = key * (2 * D) + (pc ^ swap_of<D>(key)) * 16 + 8 * (lane & 1);
-  }
+  v_offsets<D>(off, lane);
   load_k<D, E8>(t, part(first), key0(first), shift, lane);
   load_v<D, E8>(t, part(first), key0(first), shift, lane);
   for (int i = first; i < last; i += step) {
@@ -148,41 +111,10 @@ __device__ __forceinline__ void stream(Rows<D>& st, const bf16x8 (&q)[D / 16], c
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = acc_key(v, h) < left ? s[v] : -kInf;
     }
-    float mx = s[0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    mx = fmaxf(mx, other_half(mx)) * scale;
-    if (__any(mx > st.ref + kSlack)) {
-      const float ref = fmaxf(st.ref, mx);
-      const float f = st.ref == -kInf ? 0.f : fast_exp2(st.ref - ref);
-      st.ref = ref;
-      st.sum *= f;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) st.o[db][v] *= f;
-    }
-    const float ref = st.ref == -kInf ? 0.f : st.ref;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s[v] = fast_exp2(fmaf(s[v], scale, -ref));
-      st.sum += s[v];
-    }
+    weigh<D, 1>(st, &s, scale);
     v_to_lds<D, E8>(t, lds, lane);
     load_v<D, E8>(t, part(next), key0(next), shift, lane);
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      bf16x8 pf;
-#pragma unroll
-      for (int v = 0; v < 8; ++v) pf[v] = static_cast<__bf16>(s[8 * b + v]);
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b) * (2 * D)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b + 8) * (2 * D)));
-        const s16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf, st.o[db], 0, 0, 0);
-      }
-    }
+    add_values<D, 1>(st, &s, lds, off);
   }
 }
 
@@ -198,7 +130,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
   const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = rest % prm.row_tiles, split = rest / prm.row_tiles;
   const Seen pb(prm, p);
   const int r0 = rt * kRowsTile;
-  if (r0 >= pb.R) return;
+  if (!pb.has(prm, r0)) return;
   const Share sh(prm, pb, r0, kRowsTile, kRowsKeys, split);
   if (split >= sh.active) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), h = lane >> 5;
@@ -301,7 +233,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams prm, int tile_ro
   const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, ch = rest % chunks, rt = rest / chunks;
   const Seen pb(prm, p);
   const int r0 = rt * tile_rows;
-  if (r0 + ch * 32 >= pb.R) return;
+  if (!pb.has(prm, r0 + ch * 32)) return;
   const Share sh(prm, pb, r0, tile_rows, tile_keys, 0);
   if (sh.active == 1) return;
   const int rows = min(min(32, tile_rows - ch * 32), pb.R - r0 - ch * 32);
