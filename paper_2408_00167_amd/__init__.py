@@ -601,7 +601,9 @@ class Finch:
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2408_00167_amd needs a GPU: there is no CPU fallback")
         self.device = torch.device(device)
-        self.ctx = finch_create(dtype, head_dim, group_size)
+        self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        with torch.cuda.device(self.index):  # (a context is bound to the device that is current when it is made)
+            self.ctx = finch_create(dtype, head_dim, group_size)
         self.ws = None
         self.key = (torch.bfloat16 if dtype == FINCH_BF16 else torch.float32, head_dim, group_size)
         self.scale_block = 64
@@ -706,8 +708,9 @@ class Finch:
             raise ValueError(f"{what}: batch of {key}, context of {self.key}")
 
     def _stream(self, stream):
+        """The stream's handle; the current one's without the 3 us that an object for it takes."""
         import torch
-        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
+        return torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream
 
     def rotate(self, batch: RowsBatch, how: Rotary, stream=None):
         """Norm, rotary embedding and placing of projected rows."""

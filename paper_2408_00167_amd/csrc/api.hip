@@ -24,6 +24,7 @@ namespace {
 using finch::LaunchParams;
 using finch::align_up;
 using finch::aligned;
+using finch::being_captured;
 using finch::hip_fail;
 using finch::overlaps;
 
@@ -308,26 +309,16 @@ struct CaptureUnaffected {
 
 // Meeting words for the eager launches of a context, cleared (they keep themselves in order from
 // then on).  On a stream of the library's: the null stream would wait for others.
-hipError_t make_meet(int32_t** out, hipStream_t s) {
+hipError_t make_meet(int32_t** out, int words, hipStream_t s) {
   const CaptureUnaffected guard;
-  hipError_t e = hipMalloc(reinterpret_cast<void**>(out), sizeof(int32_t) * finch::kClusterMeetWords);
-  if (e == hipSuccess) e = finch::launch_zero_words(*out, finch::kClusterMeetWords, nullptr, s);
+  hipError_t e = hipMalloc(reinterpret_cast<void**>(out), sizeof(int32_t) * words);
+  if (e == hipSuccess) e = finch::launch_zero_words(*out, words, nullptr, s);
   return e == hipSuccess ? hipStreamSynchronize(s) : e;
 }
 void free_meet(int32_t* meet) {  // (waits for the device: launches may still be using them)
   if (!meet) return;
   const CaptureUnaffected guard;
   (void)hipFree(meet);
-}
-
-// Whether what is launched on `s` now is recorded into a graph (or cannot be told).
-bool being_captured(hipStream_t s) {
-  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &status) != hipSuccess) {
-    (void)hipGetLastError();
-    return true;
-  }
-  return status != hipStreamCaptureStatusNone;
 }
 
 constexpr int kProfPairs = 8192;
@@ -888,6 +879,7 @@ finch_status finch_create(const finch_config* cfg, finch_ctx** out) {
   ctx->loop_ways = nullptr;
   ctx->scale_block = 64;
   ctx->meet = nullptr;
+  ctx->attend_meet = nullptr;
   hipError_t e = hipGetDevice(&ctx->device);
   StaticAddresses a = {nullptr, nullptr, nullptr};
   if (e == hipSuccess) {
@@ -911,7 +903,8 @@ finch_status finch_create(const finch_config* cfg, finch_ctx** out) {
   if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = finch::set_max_lds_owner_doc(ctx->max_lds);
   if (e == hipSuccess && cfg->dtype == FINCH_F32) e = finch::set_max_lds_owner_f32(ctx->max_lds);
   if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = finch::set_max_lds_cluster(ctx->max_lds);
-  if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = make_meet(&ctx->meet, a.stream);
+  if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = make_meet(&ctx->meet, finch::kClusterMeetWords, a.stream);
+  if (e == hipSuccess) e = make_meet(&ctx->attend_meet, finch::kAttendMeetWords, a.stream);
   if (e == hipSuccess) e = finch::set_max_lds_select(ctx->max_lds);
   if (e == hipSuccess && cfg->dtype == FINCH_BF16) e = finch::set_max_lds_attend();
   // the re-positioning kernel also has a little static LDS
@@ -922,6 +915,7 @@ finch_status finch_create(const finch_config* cfg, finch_ctx** out) {
                  hipGetErrorString(e));
     (void)hipGetLastError();
     free_meet(ctx->meet);
+    free_meet(ctx->attend_meet);
     delete ctx;
     return FINCH_ERR_HIP;
   }
@@ -933,6 +927,7 @@ finch_status finch_destroy(finch_ctx* ctx) {
   if (ctx) {
     (void)finch_profile(ctx, 0);
     free_meet(ctx->meet);
+    free_meet(ctx->attend_meet);
   }
   delete ctx;
   return FINCH_OK;

@@ -69,7 +69,7 @@ constexpr int32_t kMostHeads = 1 << 12;
 struct AttendPlan {
   struct Part {
     int tile_rows, tile_keys;
-    int rows_lo = 0, rows_hi = 0, row_tiles = 0;  // (no row tiles: nothing to launch)
+    int rows_lo = 0, rows_hi = 0, row_tiles = 0, rows_max = 0;  // (no row tiles: nothing to launch)
     int64_t splits = 1, span = 1;
     size_t off_o = 0, off_ml = 0;
     // of its problems: tiles of rows, tiles of keys that these see, most tiles of keys
@@ -114,6 +114,7 @@ void count(AttendPlan::Part& pt, const finch_attention& a, int64_t rows) {
   const int64_t keys = cache + (a.m + pt.tile_keys - 1) / pt.tile_keys;
   if (tiles > pt.row_tiles) pt.row_tiles = static_cast<int>(tiles);
   if (keys > pt.keys_max) pt.keys_max = keys;
+  if (rows > pt.rows_max) pt.rows_max = static_cast<int>(rows);
   pt.tiles += tiles;
   // (causal rows of the chunk itself see half of themselves on average)
   const int64_t own = a.causal ? std::min(a.n_que, a.m) / 2 / pt.tile_keys : 0;
@@ -161,7 +162,11 @@ finch_status plan_attention(const finch_ctx* ctx, const finch_attention* hd, int
     const int64_t rows = int64_t{hd[i].n_que} * G;
     if (rows > 0) count(rows <= pl.few.rows_hi ? pl.few : pl.many, hd[i], rows);
   }
-  finch_status st = split(pl.few, n, 4 * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
+  // Few rows: two workgroups a compute unit are on the chip at once, and as many are enough where they are alike or few (one request,
+  // 131000 keys in 8 bits: 60 us, 73 with twice as many; 512 problems of 2000 keys 92 and 108 us); problems of different
+  // length level out with twice as many (512 of 64 to 8192 keys 224 us, 236 with half).
+  const bool alike = 4 * pl.few.keys_max * pl.few.tiles <= 5 * pl.few.work || pl.few.tiles < cu;
+  finch_status st = split(pl.few, n, (alike ? 2 : 4) * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
   if (st == FINCH_OK) st = split(pl.many, n, 2 * cu, 8, cu, ctx->cfg.head_dim, pl.bytes);
   return st;
 }
@@ -330,13 +335,16 @@ finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, cons
     p.block_shift = __builtin_ctz(static_cast<unsigned>(ctx->scale_block));
     p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(d)));
     p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pt->off_o);
+    // (a graph outlives its context, and graphs may run side by side: what is captured joins by a launch of its own)
+    const bool meets = pt != &pl.many && pt->splits > 1 && int64_t{n} * pt->row_tiles <= finch::kAttendMeetWords && !finch::being_captured(s);
+    p.meet = meets ? ctx->attend_meet : nullptr;
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + pt->off_ml);
     if (e == hipSuccess) {
       e = pt == &pl.many ? finch::launch_attend_tiles(d, pl.eight, p, s)
           : bf16         ? finch::launch_attend_rows(d, pl.eight, p, s)
                          : finch::launch_attend_rows_f32(d, p, s);
     }
-    if (e == hipSuccess && pt->splits > 1) e = finch::launch_attend_join(d, bf16, pt->tile_rows, pt->tile_keys, p, s);
+    if (e == hipSuccess && pt->splits > 1 && !meets) e = finch::launch_attend_join(d, bf16, pt->tile_rows, pt->tile_keys, pt->rows_max, p, s);
   }
   return done(ctx, e);
 }

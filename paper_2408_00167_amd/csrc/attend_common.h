@@ -31,12 +31,14 @@ struct AttendParams {
   int32_t block_shift;  // log2 of the rows per power of two of an 8-bit cache
   float scale_log2;     // log2(e) / sqrt(d_k)
   float* part;          // [n][row_tiles][splits][rows of a tile][D] sums of weighted values ...
+  int32_t* meet;        // a counter per problem and tile of rows, at zero between launches: the last split to come joins them; null: attend_join
   float2* part_ml;      // ... and [n][row_tiles][splits][rows of a tile] (reference, sum of weights)
 };
 
 // rows and keys of a tile
 constexpr int kRowsTile = 32, kRowsKeys = 32, kRowsWaves = 4;    // attend_rows
 constexpr int kF32Tile = 16, kF32Keys = 16, kF32Waves = 4;       // attend_rows_f32
+constexpr int kJoinThreads = 256;
 constexpr int kTilesRows = 256, kTilesKeys = 64, kTilesWaves = 8;  // attend_tiles
 
 __device__ __forceinline__ finch_attention load_attention(const finch_attention* p) {
@@ -97,6 +99,110 @@ __device__ __forceinline__ float other_half(float x) {
 // inside fp32 and bf16, and most tiles need no rescaling of what has been summed.
 constexpr float kSlack = 8.f;
 
-inline __device__ float from_log2(float x) { return x * 0.6931471805599453f; }
+__device__ __forceinline__ float from_log2(float x) { return x * 0.6931471805599453f; }
+
+// What a workgroup hands to another one in the same launch goes past the caches of its own part of the chip.
+__device__ __forceinline__ void to_others(void* p, f32x2 x) {
+  __hip_atomic_store(static_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void to_others(float* p, f32x4 x) {
+  to_others(p, f32x2{x[0], x[1]});
+  to_others(p + 2, f32x2{x[2], x[3]});
+}
+__device__ __forceinline__ f32x2 from_others(const void* p) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(static_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// Whether this workgroup is the last of `all` to come here, with everything they have handed over in place; called by
+// the whole workgroup.  Nobody waits for anybody.  The counter is back at zero afterwards.
+__device__ __forceinline__ bool last_to_come(int32_t* counter, int all, int tid) {
+  __shared__ int before;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's stores have arrived
+  __syncthreads();
+  if (tid == 0) before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (before != all - 1) return false;
+  if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+// Joins the splits of rows [first, first + n) of a tile that starts with stacked row r0, by a workgroup of kJoinThreads; at0: where
+// the tile's results begin.  A thread takes four channels of a row in every `groups`-th split, with a running reference, and the
+// groups are joined in LDS: few rows in many splits are read by all threads at once (131000 keys of one request in 125
+// splits took 60 us with the splits of a row behind each other).  The order of the sums depends on sizes alone.
+template <int D, bool BF16, bool HANDED>
+__device__ __forceinline__ void join_splits(const AttendParams& prm, const Seen& pb, int active, size_t at0, int tile_rows, int r0, int first, int n,
+                                            float* other, int tid) {
+  int per = kJoinThreads / (D / 4);
+  while (per > 1 && per / 2 >= n) per >>= 1;
+  const int items = per * (D / 4), groups = kJoinThreads / items, g = tid / items, it = tid % items, pc = it % (D / 4);
+  for (int b = 0; b < n; b += per) {
+    const int row = first + b + it / (D / 4), rr = r0 + row;
+    const bool there = b + it / (D / 4) < n;
+    const float2* ml = prm.part_ml + at0 + row;
+    const float* o = prm.part + (at0 + row) * D + 4 * pc;
+    float ref = -kInf, total = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    const auto add = [&](float r, float z, f32x4 y) {
+      const float to = fmaxf(ref, r), from = to == -kInf ? 0.f : to;
+      const float f0 = fast_exp2(ref - from), f1 = fast_exp2(r - from);
+      total = total * f0 + z * f1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = sum[e] * f0 + y[e] * f1;
+      ref = to;
+    };
+    if (there) {
+      constexpr int kBatch = 8;  // splits whose loads are under way together
+      for (int s0 = g; s0 < active; s0 += kBatch * groups) {
+        f32x2 w[kBatch];
+        f32x4 y[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int s = s0 + i * groups;
+          const size_t at = static_cast<size_t>(s < active ? s : s0) * tile_rows;
+          if (HANDED) {
+            w[i] = from_others(ml + at);
+            const f32x2 lo = from_others(o + at * D), hi = from_others(o + at * D + 2);
+            y[i] = f32x4{lo[0], lo[1], hi[0], hi[1]};
+          } else {
+            w[i] = *as_global<f32x2>(ml + at);
+            y[i] = *as_global<f32x4>(o + at * D);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) add(s0 + i * groups < active ? w[i][0] : -kInf, w[i][1], y[i]);
+      }
+    }
+    if (groups > 1) {
+      __syncthreads();
+      float* mine = other + tid * 6;
+      mine[0] = ref;
+      mine[1] = total;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine[2 + e] = sum[e];
+      __syncthreads();
+      if (g == 0) {
+        for (int k = 1; k < groups; ++k) {
+          const float* x = mine + k * items * 6;
+          add(x[0], x[1], f32x4{x[2], x[3], x[4], x[5]});
+        }
+      }
+    }
+    if (g > 0 || !there) continue;
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const int tok = rr / pb.group, head = rr % pb.group;
+    const long long to = tok * pb.d.out_row + head * pb.d.out_head + 4 * pc;
+    if (BF16) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(sum[e] * inv);
+      *as_global_mut<bf16x4>(static_cast<char*>(pb.d.out) + 2 * to) = y;
+    } else {
+      *as_global_mut<f32x4>(static_cast<char*>(pb.d.out) + 4 * to) = f32x4{sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+    }
+    if (pb.d.lse && pc == 0) as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(ref + fast_log2(total)) : -kInf;
+  }
+}
 
 }  // namespace finch

@@ -10,6 +10,7 @@ template <int D>
 __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams prm) {
   constexpr int kPieces = D / 16, kVals = D / 4, kQuarter = kVals / kF32Waves;
   __shared__ float ex[kF32Waves * 3 * kQuarter * 64];
+  static_assert(kF32Waves * 3 * kQuarter * 64 >= kJoinThreads * 6, "join_splits");
   __shared__ float ml[2][kF32Waves][kF32Tile];
   const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = rest % prm.row_tiles, split = rest / prm.row_tiles;
   const Seen pb(prm, p);
@@ -120,23 +121,30 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
 #pragma unroll
     for (int w = 0; w < 3; ++w) own[x] += from[w * kQuarter * 64];
   }
-  if (r0 + row >= pb.R) return;
-  const bool whole = sh.active == 1;
-  const float inv = whole ? (total > 0.f ? 1.f / total : 0.f) : 1.f;
+  const bool there = r0 + row < pb.R, whole = sh.active == 1;
   const size_t at = ((static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits + split) * kF32Tile + row;
-  float* to = whole ? static_cast<float*>(pb.d.out) + tok * pb.d.out_row + head * pb.d.out_head : prm.part + at * D;
+  if (there) {
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    float* to = static_cast<float*>(pb.d.out) + tok * pb.d.out_row + head * pb.d.out_head;
 #pragma unroll
-  for (int x = 0; x < kQuarter; x += 4) {
-    const int d = 16 * ((wave * kQuarter + x) >> 2) + 4 * part;
-    *as_global_mut<f32x4>(to + d) = f32x4{own[x] * inv, own[x + 1] * inv, own[x + 2] * inv, own[x + 3] * inv};
-  }
-  if (wave == 0 && part == 0) {
-    if (!whole) {
-      *as_global_mut<f32x2>(prm.part_ml + at) = f32x2{top, total};
-    } else if (pb.d.lse) {
-      as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
+    for (int x = 0; x < kQuarter; x += 4) {
+      const int d = 16 * ((wave * kQuarter + x) >> 2) + 4 * part;
+      if (whole) {
+        *as_global_mut<f32x4>(to + d) = f32x4{own[x] * inv, own[x + 1] * inv, own[x + 2] * inv, own[x + 3] * inv};
+      } else {
+        to_others(prm.part + at * D + d, f32x4{own[x], own[x + 1], own[x + 2], own[x + 3]});
+      }
+    }
+    if (wave == 0 && part == 0) {
+      if (!whole) {
+        to_others(prm.part_ml + at, f32x2{top, total});
+      } else if (pb.d.lse) {
+        as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
+      }
     }
   }
+  if (!whole && prm.meet && last_to_come(prm.meet + p * prm.row_tiles + rt, sh.active, tid))
+    join_splits<D, false, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kF32Tile, kF32Tile, r0, 0, min(kF32Tile, pb.R - r0), ex, tid);
 }
 
 hipError_t launch_attend_rows_f32(int head_dim, const AttendParams& p, hipStream_t s) {

@@ -14,6 +14,8 @@
 // the softmax's reference is a multiplication by one number a lane.
 //
 // K of the next tile is under way while the softmax runs, V of the next tile during P V.
+#include <algorithm>
+
 #include "attend.h"
 #include "attend_bf16.h"
 
@@ -200,8 +202,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
 #pragma unroll
     for (int w = 0; w < 3; ++w) own[x] += from[w * kQuarter * 64];
   }
-  if (r0 + row >= pb.R) return;
+  const bool there = r0 + row < pb.R;
   if (sh.active == 1) {
+    if (!there) return;
     const float inv = total > 0.f ? 1.f / total : 0.f;
     char* to = static_cast<char*>(pb.d.out) + (tok * pb.d.out_row + head * pb.d.out_head) * 2;
 #pragma unroll
@@ -217,58 +220,31 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
       as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
   } else {
     const size_t at = ((static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits + split) * kRowsTile + row;
-    float* to = prm.part + at * D;
+    if (there) {
 #pragma unroll
-    for (int x = 0; x < kQuarter; x += 4) {
-      const int v = wave * kQuarter + x, d = 32 * (v >> 4) + 8 * ((v & 15) >> 2) + 4 * h;
-      *as_global_mut<f32x4>(to + d) = f32x4{own[x], own[x + 1], own[x + 2], own[x + 3]};
+      for (int x = 0; x < kQuarter; x += 4) {
+        const int v = wave * kQuarter + x, d = 32 * (v >> 4) + 8 * ((v & 15) >> 2) + 4 * h;
+        to_others(prm.part + at * D + d, f32x4{own[x], own[x + 1], own[x + 2], own[x + 3]});
+      }
+      if (wave == 0 && h == 0) to_others(prm.part_ml + at, f32x2{top, total});
     }
-    if (wave == 0 && h == 0) *as_global_mut<f32x2>(prm.part_ml + at) = f32x2{top, total};
+    if (prm.meet && last_to_come(prm.meet + p * prm.row_tiles + rt, sh.active, tid))
+      join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRowsTile, kRowsTile, r0, 0, min(kRowsTile, pb.R - r0), ex, tid);
   }
 }
 
-// Joins the splits of a tile of rows: one workgroup for 32 of its rows (fewer if the tile has fewer).
+// Joins the splits of `per` rows of a tile of rows (see join_splits).
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void attend_join(AttendParams prm, int tile_rows, int tile_keys, int chunks) {
+__global__ __launch_bounds__(kJoinThreads) void attend_join(AttendParams prm, int tile_rows, int tile_keys, int per, int chunks) {
+  __shared__ float other[kJoinThreads * 6];
   const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, ch = rest % chunks, rt = rest / chunks;
   const Seen pb(prm, p);
   const int r0 = rt * tile_rows;
-  if (!pb.has(prm, r0 + ch * 32)) return;
+  if (!pb.has(prm, r0 + ch * per)) return;
   const Share sh(prm, pb, r0, tile_rows, tile_keys, 0);
   if (sh.active == 1) return;
-  const int rows = min(min(32, tile_rows - ch * 32), pb.R - r0 - ch * 32);
-  for (int it = threadIdx.x; it < rows * (D / 4); it += 256) {
-    const int row = ch * 32 + it / (D / 4), pc = it % (D / 4);
-    const size_t at = (static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits * tile_rows + row;
-    const FINCH_GLOBAL f32x2* ml = as_global<f32x2>(prm.part_ml + at);
-    const FINCH_GLOBAL f32x4* o = as_global<f32x4>(prm.part + at * D) + pc;
-    float top = -kInf;
-    for (int s = 0; s < sh.active; ++s) top = fmaxf(top, ml[static_cast<size_t>(s) * tile_rows][0]);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < sh.active; ++s) {
-      const f32x2 w = ml[static_cast<size_t>(s) * tile_rows];
-      const float f = w[0] == -kInf ? 0.f : fast_exp2(w[0] - top);
-      const f32x4 y = o[static_cast<size_t>(s) * tile_rows * (D / 4)];
-      total += w[1] * f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
-    }
-    const float inv = total > 0.f ? 1.f / total : 0.f;
-    const int rr = r0 + row, tok = rr / pb.group, head = rr % pb.group;
-    const long long at_out = tok * pb.d.out_row + head * pb.d.out_head + 4 * pc;
-    if (BF16) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      bf16x4 y;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(sum[e] * inv);
-      *as_global_mut<bf16x4>(static_cast<char*>(pb.d.out) + 2 * at_out) = y;
-    } else {
-      *as_global_mut<f32x4>(static_cast<char*>(pb.d.out) + 4 * at_out) = f32x4{sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
-    }
-    if (pb.d.lse && pc == 0) as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
-  }
+  join_splits<D, BF16, false>(prm, pb, sh.active, (static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits * tile_rows, tile_rows, r0, ch * per,
+                              min(per, pb.R - r0 - ch * per), other, threadIdx.x);
 }
 
 hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, hipStream_t s) {
@@ -285,17 +261,18 @@ hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, h
   return hipGetLastError();
 }
 
-hipError_t launch_attend_join(int head_dim, bool bf16, int tile_rows, int tile_keys, const AttendParams& p, hipStream_t s) {
-  const int chunks = (tile_rows + 31) / 32;
-  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * chunks), block(256);
+hipError_t launch_attend_join(int head_dim, bool bf16, int tile_rows, int tile_keys, int rows_max, const AttendParams& p, hipStream_t s) {
+  const int per = p.splits >= 16 && static_cast<int64_t>(p.n) * rows_max <= 2048 ? 1 : 8;
+  const int chunks = (std::min(rows_max, tile_rows) + per - 1) / per;  // of a tile of rows
+  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * chunks), block(kJoinThreads);
   if (head_dim == 128 && bf16) {
-    hipLaunchKernelGGL((attend_join<128, true>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+    hipLaunchKernelGGL((attend_join<128, true>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
   } else if (head_dim == 128) {
-    hipLaunchKernelGGL((attend_join<128, false>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+    hipLaunchKernelGGL((attend_join<128, false>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
   } else if (bf16) {
-    hipLaunchKernelGGL((attend_join<64, true>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+    hipLaunchKernelGGL((attend_join<64, true>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
   } else {
-    hipLaunchKernelGGL((attend_join<64, false>), grid, block, 0, s, p, tile_rows, tile_keys, chunks);
+    hipLaunchKernelGGL((attend_join<64, false>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
   }
   return hipGetLastError();
 }

@@ -32,6 +32,7 @@ struct finch_ctx {
   bool loop_checked;
   bool loop_rows_may_stay;  // what check_slot_overlaps said of that set
   int32_t* loop_ways;       // LaunchParams::ways of its whole loops
+  int32_t* attend_meet;     // counters of finch_attend's launches (attend_common.h)
   int scale_block;          // rows per power of two of an 8-bit cache
 };
 
@@ -44,6 +45,16 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   if (!a || !b || na == 0 || nb == 0) return false;
   const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
   return a0 < b0 + nb && b0 < a0 + na;
+}
+
+// Whether what is launched on `s` now is recorded into a graph (or cannot be told).
+inline bool being_captured(hipStream_t s) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &status) != hipSuccess) {
+    (void)hipGetLastError();
+    return true;
+  }
+  return status != hipStreamCaptureStatusNone;
 }
 
 inline finch_status hip_fail(finch_ctx* ctx, hipError_t e) {

@@ -38,6 +38,8 @@ constexpr int kClusterMaxKeys = 15872;  // what a 512-thread selection holds in 
 constexpr int kClusterMaxRows = 4096;
 // Words in which the workgroups of such a launch meet.
 constexpr int kClusterMeetWords = 32 + 18 * kMaxClusterGrid;
+// Counters in which the splits of a tile of rows meet (finch_attend, launches outside of captures).
+constexpr int kAttendMeetWords = 8192;
 // A workgroup that has waited for others this long in all (100 MHz ticks) does their work itself:
 // 0.1 ms, and 1 us for every tile of 32 keys x 32 rows of a slice.  Both passes over a tile take
 // 0.22 us (128 channels, 304 tiles: 66 us), so slices that differ in length, or workgroups that
