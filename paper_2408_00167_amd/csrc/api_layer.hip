@@ -126,6 +126,8 @@ void count(AttendPlan::Part& pt, const finch_attention& a, int64_t rows) {
 finch_status split(AttendPlan::Part& pt, int64_t n, int64_t groups, int64_t span_min, int64_t enough, int head_dim, size_t& off) {
   const int64_t tiles = n * pt.row_tiles, part = int64_t{pt.tile_rows} * (head_dim + 2) * 4;
   if (tiles == 0) return FINCH_OK;
+  // (a join takes its time with the number of splits, so that it is shortest with the square root of all tiles)
+  span_min = std::max(span_min, static_cast<int64_t>(std::sqrt(0.5 * static_cast<double>(pt.keys_max))));
   pt.span = std::max((pt.work + groups - 1) / groups, span_min);
   if (pt.tiles >= enough) pt.span = std::max<int64_t>(pt.keys_max, 1);
   // (partial results of at most 64 MiB and 2^15 tiles of rows)

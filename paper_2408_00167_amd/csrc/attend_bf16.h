@@ -39,17 +39,38 @@ struct Rows {
   f32x16 o[D / 32];
 };
 
-// Logits of one row against NB blocks of 32 keys become weights: the maximum moves the reference if it is far above it,
-// the weights' sum goes to the lane's.
+// Logits of one row against NB blocks of 32 keys become weights, as the B operands of steps of 16 keys (the one rounding they
+// get), and their sum goes to the lane's.  The reference only has to keep the weights in range, and neither fp32 nor bf16 lose
+// anything for weights far above one: it is taken from the row's first tile and moved only when a tile's sum in some lane passes
+// 2^kSlack, so that most tiles need no maximum.
 template <int D, int NB>
-__device__ __forceinline__ void weigh(Rows<D>& st, f32x16* s, float scale) {
-  float mx = s[0][0];
+__device__ __forceinline__ void weigh(Rows<D>& st, const f32x16* s, bf16x8* pf, float scale) {
+  float part[4];
+  const auto pass = [&](float ref) {
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb)
+    for (int i = 0; i < 4; ++i) part[i] = 0.f;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
-  mx = fmaxf(mx, other_half(mx)) * scale;
-  if (__any(mx > st.ref + kSlack)) {
+    for (int b = 0; b < 2 * NB; ++b)
+#pragma unroll
+      for (int v = 0; v < 8; ++v) {
+        const float w = fast_exp2(fmaf(s[b >> 1][8 * (b & 1) + v], scale, -ref));
+        part[v & 3] += w;
+        pf[b][v] = static_cast<__bf16>(w);
+      }
+    part[0] = (part[0] + part[1]) + (part[2] + part[3]);
+  };
+  bool move = __any(st.ref == -kInf);
+  if (!move) {
+    pass(st.ref);
+    move = __any(!(part[0] <= __builtin_exp2f(kSlack)));
+  }
+  if (move) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+    mx = fmaxf(mx, other_half(mx)) * scale;
     const float ref = fmaxf(st.ref, mx);
     const float f = st.ref == -kInf ? 0.f : fast_exp2(st.ref - ref);
     st.ref = ref;
@@ -58,15 +79,9 @@ __device__ __forceinline__ void weigh(Rows<D>& st, f32x16* s, float scale) {
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int v = 0; v < 16; ++v) st.o[db][v] *= f;
+    pass(ref == -kInf ? 0.f : ref);
   }
-  const float ref = st.ref == -kInf ? 0.f : st.ref;
-#pragma unroll
-  for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s[kb][v] = fast_exp2(fmaf(s[kb][v], scale, -ref));
-      st.sum += s[kb][v];
-    }
+  st.sum += part[0];
 }
 
 // Where a lane reads V^T in LDS: keys 4h + (lane & 15) / 4 of a step of 16, columns of its 16-lane group.
@@ -81,18 +96,15 @@ __device__ __forceinline__ void v_offsets(int (&off)[D / 32], int lane) {
 
 // O^T += V^T P^T for NB blocks of 32 keys.
 template <int D, int NB>
-__device__ __forceinline__ void add_values(Rows<D>& st, const f32x16* s, const char* lds, const int (&off)[D / 32]) {
+__device__ __forceinline__ void add_values(Rows<D>& st, const bf16x8* pf, const char* lds, const int (&off)[D / 32]) {
 #pragma unroll
   for (int b = 0; b < 2 * NB; ++b) {
-    bf16x8 pf;
-#pragma unroll
-    for (int v = 0; v < 8; ++v) pf[v] = static_cast<__bf16>(s[b >> 1][8 * (b & 1) + v]);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) {
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b) * (2 * D)));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(lds + off[db] + (16 * b + 8) * (2 * D)));
       const s16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf, st.o[db], 0, 0, 0);
+      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf[b], st.o[db], 0, 0, 0);
     }
   }
 }

@@ -95,9 +95,9 @@ __device__ __forceinline__ float other_half(float x) {
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// Weights may stand up to 2^kSlack above the reference before it is moved: sums stay far
-// inside fp32 and bf16, and most tiles need no rescaling of what has been summed.
-constexpr float kSlack = 8.f;
+// How far weights may stand above the reference (log2) before it is moved: the sums of 2^24 of them stay far
+// inside fp32.
+constexpr float kSlack = 16.f;
 
 __device__ __forceinline__ float from_log2(float x) { return x * 0.6931471805599453f; }
 

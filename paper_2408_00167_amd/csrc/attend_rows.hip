@@ -113,10 +113,11 @@ __device__ __forceinline__ void stream(Rows<D>& st, const bf16x8 (&q)[D / 16], c
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = acc_key(v, h) < left ? s[v] : -kInf;
     }
-    weigh<D, 1>(st, &s, scale);
+    bf16x8 pf[2];
+    weigh<D, 1>(st, &s, pf, scale);
     v_to_lds<D, E8>(t, lds, lane);
     load_v<D, E8>(t, part(next), key0(next), shift, lane);
-    add_values<D, 1>(st, &s, lds, off);
+    add_values<D, 1>(st, pf, lds, off);
   }
 }
 

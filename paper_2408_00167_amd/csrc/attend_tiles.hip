@@ -1,9 +1,13 @@
 // Attention of many rows, bf16: 256 stacked rows a workgroup, 32 for each of its eight waves, which walk
-// the keys together in tiles of 64.  K and V of a tile lie in LDS, where all waves read them; the next
-// tile is on its way from memory to registers meanwhile and goes to a second pair of buffers behind the products, so
-// that there is one barrier a tile.  The calculation of a wave is that of attend_rows: S^T = K Q^T, a
+// the keys together in tiles of 64.  K and V of a tile lie in LDS, where all waves read them, in two buffers each; what
+// comes next is on its way from memory to registers meanwhile.  The calculation of a wave is that of attend_rows: S^T = K Q^T, a
 // running softmax of a lane's own row, O^T = V^T P^T.  Rows, splits and joins are those of attend_common.h; the tiles
 // with the most keys start first.
+//
+// A tile costs a wave as many cycles of the matrix pipe (32 products) as of the vector unit (32 exponentials a lane and what
+// belongs to them), so the two waves of a SIMD take turns: the first four waves make their products - S of the next
+// tile and P V of this one - while the others weigh, and the other way round, with a barrier at each change.  All
+// eight in step left both pipes idle half of the time (4096 rows of 32 heads on 1364 kept rows of 8: 235 us).
 #include "attend.h"
 #include "attend_bf16.h"
 
@@ -13,59 +17,45 @@ namespace {
 
 constexpr int kThreads = 64 * kTilesWaves;
 
-// A tile of K and V between memory and LDS: this thread's pieces.
+// A tile of K or of V between memory and LDS: this thread's 16-byte pieces, of bf16 or of e4m3.
 template <int D>
 struct Staged {
-  static constexpr int kMine = kTilesKeys * (D / 8) / kThreads;  // 16-byte pieces of bf16, of K and of V
-  u32x4 k[kMine], v[kMine];
-  unsigned ks, vs;
+  static constexpr int kMine = kTilesKeys * (D / 8) / kThreads, kMine8 = (kMine + 1) / 2;
+  u32x4 x[kMine];
+  unsigned e[kMine8];
 };
 
-// Row r of a tile in LDS starts with piece r & 15 (& 7) of K, so that 16 (8) rows read side by side are clear of each other.
-template <int D>
-__device__ __forceinline__ int k_swap(int r) {
-  return r & (D / 8 - 1);
+// Row r of a tile in LDS starts with piece r & 15 (& 7) of K, so that 16 (8) rows read side by side are clear of each other;
+// V as swap_of says.
+template <int D, bool V>
+__device__ __forceinline__ int swap_in(int r) {
+  return V ? swap_of<D>(r) : r & (D / 8 - 1);
 }
 
 template <int D, bool E8>
-__device__ __forceinline__ void fetch(Staged<D>& t, const Part& a, int key0, int shift, int tid) {
-  if (E8) {
-    constexpr int kPer = D / 16;  // pieces of 16 e4m3 numbers
-    const int key = min(key0 + min(tid / kPer, kTilesKeys - 1), a.n - 1);
-    t.k[0] = as_global<u32x4>(a.k + key * a.row)[tid % kPer];
-    t.v[0] = as_global<u32x4>(a.v + key * a.row)[tid % kPer];
-    t.ks = as_global<unsigned char>(a.ks)[key >> shift];
-    t.vs = as_global<unsigned char>(a.vs)[key >> shift];
-  } else {
-    constexpr int kPer = D / 8;
+__device__ __forceinline__ void fetch(Staged<D>& t, const char* rows, long long row, int n, const unsigned char* exps, int key0, int shift, int tid) {
+  constexpr int kPer = D / (E8 ? 16 : 8);  // pieces of a row
 #pragma unroll
-    for (int i = 0; i < Staged<D>::kMine; ++i) {
-      const int id = i * kThreads + tid, key = min(key0 + id / kPer, a.n - 1);
-      t.k[i] = as_global<u32x4>(a.k + key * a.row)[id % kPer];
-      t.v[i] = as_global<u32x4>(a.v + key * a.row)[id % kPer];
-    }
+  for (int i = 0; i < (E8 ? Staged<D>::kMine8 : Staged<D>::kMine); ++i) {
+    const int id = i * kThreads + tid, key = min(key0 + min(id / kPer, kTilesKeys - 1), n - 1);
+    t.x[i] = as_global<u32x4>(rows + key * row)[id % kPer];
+    if (E8) t.e[i] = as_global<unsigned char>(exps)[key >> shift];
   }
 }
 
-template <int D, bool E8>
-__device__ __forceinline__ void store(const Staged<D>& t, char* lds_k, char* lds_v, int tid) {
-  if (E8) {
-    constexpr int kPer = D / 16;
-    const int r = tid / kPer, pc = 2 * (tid % kPer);
-    if (kPer * kTilesKeys < kThreads && r >= kTilesKeys) return;
-    char* k = lds_k + r * (2 * D);
-    char* v = lds_v + r * (2 * D);
-    *reinterpret_cast<bf16x8*>(k + (pc ^ k_swap<D>(r)) * 16) = widen(t.k[0][0], t.k[0][1], t.ks);
-    *reinterpret_cast<bf16x8*>(k + ((pc + 1) ^ k_swap<D>(r)) * 16) = widen(t.k[0][2], t.k[0][3], t.ks);
-    *reinterpret_cast<bf16x8*>(v + (pc ^ swap_of<D>(r)) * 16) = widen(t.v[0][0], t.v[0][1], t.vs);
-    *reinterpret_cast<bf16x8*>(v + ((pc + 1) ^ swap_of<D>(r)) * 16) = widen(t.v[0][2], t.v[0][3], t.vs);
-  } else {
-    constexpr int kPer = D / 8;
+template <int D, bool E8, bool V>
+__device__ __forceinline__ void store(const Staged<D>& t, char* lds, int tid) {
+  constexpr int kPer = D / (E8 ? 16 : 8);
 #pragma unroll
-    for (int i = 0; i < Staged<D>::kMine; ++i) {
-      const int id = i * kThreads + tid, r = id / kPer, pc = id % kPer;
-      *reinterpret_cast<u32x4*>(lds_k + r * (2 * D) + (pc ^ k_swap<D>(r)) * 16) = t.k[i];
-      *reinterpret_cast<u32x4*>(lds_v + r * (2 * D) + (pc ^ swap_of<D>(r)) * 16) = t.v[i];
+  for (int i = 0; i < (E8 ? Staged<D>::kMine8 : Staged<D>::kMine); ++i) {
+    const int id = i * kThreads + tid, r = id / kPer, pc = id % kPer;
+    if (kPer * kTilesKeys < kThreads && r >= kTilesKeys) return;
+    char* to = lds + r * (2 * D);
+    if (E8) {
+      *reinterpret_cast<bf16x8*>(to + ((2 * pc) ^ swap_in<D, V>(r)) * 16) = widen(t.x[i][0], t.x[i][1], t.e[i]);
+      *reinterpret_cast<bf16x8*>(to + ((2 * pc + 1) ^ swap_in<D, V>(r)) * 16) = widen(t.x[i][2], t.x[i][3], t.e[i]);
+    } else {
+      *reinterpret_cast<u32x4*>(to + (pc ^ swap_in<D, V>(r)) * 16) = t.x[i];
     }
   }
 }
@@ -75,7 +65,7 @@ __device__ __forceinline__ void store(const Staged<D>& t, char* lds_k, char* lds
 template <int D, bool EIGHT>
 __global__ __launch_bounds__(kThreads, 2) void attend_tiles(AttendParams prm) {
   constexpr int kBuf = kTilesKeys * D * 2;
-  extern __shared__ __align__(16) char lds[];  // [2][K, V]
+  extern __shared__ __align__(16) char lds[];  // two tiles of K, two of V
   const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = prm.row_tiles - 1 - rest % prm.row_tiles, split = rest / prm.row_tiles;
   const Seen pb(prm, p);
   const int r0 = rt * kTilesRows;
@@ -104,63 +94,110 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(AttendParams prm) {
     for (int v = 0; v < 16; ++v) st.o[db][v] = 0.f;
   // what the row, the first and the last row of the wave see
   const int lim = pb.limit(rr), lim_all = uni(pb.limit(min(w0, pb.R - 1))), lim_any = uni(pb.limit(min(w0 + 31, pb.R - 1)));
-  const bool idle = w0 >= pb.R;
   int voff[D / 32], koff[D / 16];
   v_offsets<D>(voff, lane);
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) koff[s] = row * (2 * D) + ((4 * (s >> 1) + 2 * h + (s & 1)) ^ k_swap<D>(row)) * 16;
-  Staged<D> t;
-  const auto get = [&](int i) {
+  for (int s = 0; s < D / 16; ++s) koff[s] = row * (2 * D) + ((4 * (s >> 1) + 2 * h + (s & 1)) ^ swap_in<D, false>(row)) * 16;
+  // tiles are numbered from the split's first on; the wave sees the first `mine` of them
+  const int all = sh.last - sh.first, late = wave >> 2;
+  const int seen = (min(lim_any, cache.n) + kTilesKeys - 1) / kTilesKeys + (max(lim_any - cache.n, 0) + kTilesKeys - 1) / kTilesKeys;
+  const int mine = w0 < pb.R ? min(seen - sh.first, all) : 0;
+  char* const lds_v = lds + 2 * kBuf;
+  Staged<D> tk, tv;
+  const auto get = [&](Staged<D>& t, int j, bool v) {
+    if (j >= all) return;
+    const int i = sh.first + j;
     if (EIGHT && eight && i < sh.cache_tiles) {
-      fetch<D, true>(t, cache, i * kTilesKeys, prm.block_shift, tid);
+      fetch<D, true>(t, v ? cache.v : cache.k, cache.row, cache.n, v ? cache.vs : cache.ks, i * kTilesKeys, prm.block_shift, tid);
     } else {
       const bool in_cache = i < sh.cache_tiles;
-      fetch<D, false>(t, in_cache ? cache : chunk, (in_cache ? i : i - sh.cache_tiles) * kTilesKeys, 0, tid);
+      const Part& a = in_cache ? cache : chunk;
+      fetch<D, false>(t, v ? a.v : a.k, a.row, a.n, nullptr, (in_cache ? i : i - sh.cache_tiles) * kTilesKeys, 0, tid);
     }
   };
-  const auto put = [&](int i, char* buf) {
-    if (EIGHT && eight && i < sh.cache_tiles) {
-      store<D, true>(t, buf, buf + kBuf, tid);
+  const auto put_k = [&](int j) {
+    if (j >= all) return;
+    if (EIGHT && eight && sh.first + j < sh.cache_tiles) {
+      store<D, true, false>(tk, lds + (j & 1) * kBuf, tid);
     } else {
-      store<D, false>(t, buf, buf + kBuf, tid);
+      store<D, false, false>(tk, lds + (j & 1) * kBuf, tid);
     }
   };
-  if (sh.first < sh.last) {
-    get(sh.first);
-    put(sh.first, lds);
-  }
-  __syncthreads();
-  for (int i = sh.first; i < sh.last; ++i) {
-    char* buf = lds + ((i - sh.first) & 1) * (2 * kBuf);
-    if (i + 1 < sh.last) get(i + 1);
+  const auto put_v = [&](int j) {
+    if (j >= all) return;
+    if (EIGHT && eight && sh.first + j < sh.cache_tiles) {
+      store<D, true, true>(tv, lds_v + (j & 1) * kBuf, tid);
+    } else {
+      store<D, false, true>(tv, lds_v + (j & 1) * kBuf, tid);
+    }
+  };
+  f32x16 s[2];
+  bf16x8 pf[4];
+  const auto logits = [&](int j) {
+    if (j >= mine) return;
+    const char* buf = lds + (j & 1) * kBuf;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      const bf16x8 k0 = *reinterpret_cast<const bf16x8*>(buf + koff[c]);
+      const bf16x8 k1 = *reinterpret_cast<const bf16x8*>(buf + koff[c] + 32 * (2 * D));
+      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, q[c], s[0], 0, 0, 0);
+      s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, q[c], s[1], 0, 0, 0);
+    }
+  };
+  const auto weights = [&](int j) {
+    if (j >= mine) return;
+    const int i = sh.first + j;
     const bool in_cache = i < sh.cache_tiles;
     const int base = (in_cache ? i : i - sh.cache_tiles) * kTilesKeys, before = in_cache ? 0 : cache.n, n = in_cache ? cache.n : pb.m;
-    if (!idle && base < lim_any - before) {
-      f32x16 s[2];
+    if (base + kTilesKeys > min(lim_all - before, n)) {
+      const int left = min(lim - before, n) - base;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        const bf16x8 k0 = *reinterpret_cast<const bf16x8*>(buf + koff[c]);
-        const bf16x8 k1 = *reinterpret_cast<const bf16x8*>(buf + koff[c] + 32 * (2 * D));
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, q[c], s[0], 0, 0, 0);
-        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, q[c], s[1], 0, 0, 0);
-      }
-      if (base + kTilesKeys > min(lim_all - before, n)) {
-        const int left = min(lim - before, n) - base;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) s[kb][v] = 32 * kb + acc_key(v, h) < left ? s[kb][v] : -kInf;
-      }
-      weigh<D, 2>(st, s, prm.scale_log2);
-      add_values<D, 2>(st, s, buf + kBuf, voff);
+        for (int v = 0; v < 16; ++v) s[kb][v] = 32 * kb + acc_key(v, h) < left ? s[kb][v] : -kInf;
     }
-    if (i + 1 < sh.last) put(i + 1, lds + ((i + 1 - sh.first) & 1) * (2 * kBuf));
+    weigh<D, 2>(st, s, pf, prm.scale_log2);
+  };
+  get(tk, 0, false);
+  get(tv, 0, true);
+  put_k(0);
+  put_v(0);
+  get(tk, 1, false);
+  put_k(1);
+  __syncthreads();
+  get(tk, 2, false);
+  get(tv, 1, true);
+  logits(0);
+  weights(0);
+  __syncthreads();
+  // From here on the late waves are one turn behind the others.  In turn 2j the first ones make the products with K of tile j + 1
+  // and V of tile j, in turn 2j + 1 the late ones do.  K of tile j + 2 and V of tile j + 1 go to the buffers of tiles j and
+  // j - 1, which were read last in turn 2j - 1: the late waves' part in turn 2j, the others' in turn 2j + 1.
+  if (late) {
+    put_k(2);
+    put_v(1);
+    get(tk, 3, false);
+    get(tv, 2, true);
     __syncthreads();
   }
+  for (int j = 0; j < all; ++j) {
+    __builtin_amdgcn_s_setprio(1);
+    logits(j + 1);
+    if (j < mine) add_values<D, 2>(st, pf, lds_v + (j & 1) * kBuf, voff);
+    __builtin_amdgcn_s_setprio(0);
+    __syncthreads();
+    put_k(j + 2 + late);
+    put_v(j + 1 + late);
+    get(tk, j + 3 + late, false);
+    get(tv, j + 2 + late, true);
+    weights(j + 1);
+    __syncthreads();
+  }
+  if (!late) __syncthreads();
   if (w0 + row >= pb.R) return;
   const float total = st.sum + other_half(st.sum);
   const bool whole = sh.active == 1;
