@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libfinch.so")
 PHASES_LIB_PATH = os.path.join(PKG_DIR, "libfinch_phases.so")
 
 SOURCES = ["api.hip", "score_bf16.hip", "owner_bf16.hip", "owner_once_bf16.hip", "owner_doc_bf16.hip", "cluster_bf16.hip", "owner_f32.hip", "score_f32.hip", "select.hip", "reposition.hip", "prompt_lse.hip",
-           "gather.hip", "api_layer.hip", "attend_rows.hip", "attend_tiles.hip", "attend_f32.hip", "rotate.hip", "quantize.hip"]
+           "gather.hip", "api_layer.hip", "attend_rows.hip", "attend_rows16.hip", "attend_tiles.hip", "attend_f32.hip", "rotate.hip", "quantize.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

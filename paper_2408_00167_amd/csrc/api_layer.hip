@@ -63,18 +63,23 @@ bool between_rows(const void* a, const void* b, int64_t n, int64_t row, int64_t 
 }
 
 constexpr int32_t kMostRows = 1 << 24;
+// Most stacked rows of a problem that go to attend_rows.
+constexpr int kSomeRows = 64;
 constexpr int32_t kMostHeads = 1 << 12;
 
-// How one batch of finch_attend is launched: problems of few rows and of many by kernels of their own.
+// How one batch of finch_attend is launched: problems of few rows, of some and of many by kernels of their own.
 struct AttendPlan {
   struct Part {
-    int tile_rows, tile_keys;
-    int rows_lo = 0, rows_hi = 0, row_tiles = 0, rows_max = 0;  // (no row tiles: nothing to launch)
+    int tile_rows, tile_keys, rows_lo, rows_hi;
+    int row_tiles = 0, rows_max = 0;  // (no row tiles: nothing to launch)
     int64_t splits = 1, span = 1;
     size_t off_o = 0, off_ml = 0;
     // of its problems: tiles of rows, tiles of keys that these see, most tiles of keys
     int64_t tiles = 0, work = 0, keys_max = 0;
-  } few, many;
+  };
+  Part few = {finch::kRows16, finch::kRowsKeys, 1, finch::kRows16};
+  Part some = {finch::kRowsTile, finch::kRowsKeys, finch::kRows16 + 1, kSomeRows};
+  Part many = {finch::kTilesRows, finch::kTilesKeys, kSomeRows + 1, INT32_MAX};
   bool eight = false;
   size_t bytes = 0;
 };
@@ -105,9 +110,6 @@ finch_status check_attention(const finch_ctx* ctx, const finch_attention& a) {
   }
   return FINCH_OK;
 }
-
-// Most stacked rows that go the way of few rows.
-constexpr int kFewRows = 64;
 
 void count(AttendPlan::Part& pt, const finch_attention& a, int64_t rows) {
   const int64_t tiles = (rows + pt.tile_rows - 1) / pt.tile_rows, cache = (a.c + pt.tile_keys - 1) / pt.tile_keys;
@@ -150,25 +152,22 @@ finch_status split(AttendPlan::Part& pt, int64_t n, int64_t groups, int64_t span
 finch_status plan_attention(const finch_ctx* ctx, const finch_attention* hd, int32_t n, AttendPlan& pl) {
   const bool bf16 = ctx->cfg.dtype == FINCH_BF16;
   const int G = ctx->cfg.group_size, cu = ctx->n_cu > 0 ? ctx->n_cu : 256;
-  pl.few.tile_rows = bf16 ? finch::kRowsTile : finch::kF32Tile;
-  pl.few.tile_keys = bf16 ? finch::kRowsKeys : finch::kF32Keys;
-  pl.few.rows_hi = bf16 ? kFewRows : INT32_MAX;
-  pl.many.tile_rows = finch::kTilesRows;
-  pl.many.tile_keys = finch::kTilesKeys;
-  pl.many.rows_lo = kFewRows + 1;
-  pl.many.rows_hi = INT32_MAX;
+  if (!bf16) pl.some = {finch::kF32Tile, finch::kF32Keys, 1, INT32_MAX};
   for (int32_t i = 0; i < n; ++i) {
     const finch_status st = check_attention(ctx, hd[i]);
     if (st != FINCH_OK) return st;
     if (hd[i].k_scale) pl.eight = true;
     const int64_t rows = int64_t{hd[i].n_que} * G;
-    if (rows > 0) count(rows <= pl.few.rows_hi ? pl.few : pl.many, hd[i], rows);
+    if (rows > 0) count(!bf16 ? pl.some : rows <= pl.few.rows_hi ? pl.few : rows <= pl.some.rows_hi ? pl.some : pl.many, hd[i], rows);
   }
-  // Few rows: two workgroups a compute unit are on the chip at once, and as many are enough where they are alike or few (one request,
-  // 131000 keys in 8 bits: 60 us, 73 with twice as many; 512 problems of 2000 keys 92 and 108 us); problems of different
-  // length level out with twice as many (512 of 64 to 8192 keys 224 us, 236 with half).
-  const bool alike = 4 * pl.few.keys_max * pl.few.tiles <= 5 * pl.few.work || pl.few.tiles < cu;
-  finch_status st = split(pl.few, n, (alike ? 2 : 4) * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
+  finch_status st = FINCH_OK;
+  for (AttendPlan::Part* pt : {&pl.few, &pl.some}) {
+    // Two workgroups a compute unit are on the chip at once, and as many are enough where they are alike or few (one request,
+    // 131000 keys in 8 bits: 60 us, 73 with twice as many; 512 problems of 2000 keys 92 and 108 us); problems of different
+    // length level out with twice as many (512 of 64 to 8192 keys 224 us, 236 with half).
+    const bool alike = 4 * pt->keys_max * pt->tiles <= 5 * pt->work || pt->tiles < cu;
+    if (st == FINCH_OK) st = split(*pt, n, (alike ? 2 : 4) * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
+  }
   if (st == FINCH_OK) st = split(pl.many, n, 2 * cu, 8, cu, ctx->cfg.head_dim, pl.bytes);
   return st;
 }
@@ -316,14 +315,14 @@ finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, cons
   AttendPlan pl;
   if ((st = plan_attention(ctx, host_desc, n, pl)) != FINCH_OK) return st;
   if (pl.bytes > 0 && (!ws || !aligned(ws, 256) || ws_bytes < pl.bytes)) return FINCH_ERR_WORKSPACE;
-  if (pl.few.row_tiles == 0 && pl.many.row_tiles == 0) return FINCH_OK;
+  if (pl.few.row_tiles == 0 && pl.some.row_tiles == 0 && pl.many.row_tiles == 0) return FINCH_OK;
   const OnDevice on(ctx);
   if (on.e != hipSuccess) return done(ctx, on.e);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = ctx->cfg.dtype == FINCH_BF16;
   const int d = ctx->cfg.head_dim;
   hipError_t e = hipSuccess;
-  for (const AttendPlan::Part* pt : {&pl.many, &pl.few}) {
+  for (const AttendPlan::Part* pt : {&pl.many, &pl.some, &pl.few}) {
     if (pt->row_tiles == 0) continue;
     AttendParams p;
     p.descs = dev_desc;
@@ -341,10 +340,13 @@ finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, cons
     const bool meets = pt != &pl.many && pt->splits > 1 && int64_t{n} * pt->row_tiles <= finch::kAttendMeetWords && !finch::being_captured(s);
     p.meet = meets ? ctx->attend_meet : nullptr;
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + pt->off_ml);
-    if (e == hipSuccess) {
-      e = pt == &pl.many ? finch::launch_attend_tiles(d, pl.eight, p, s)
-          : bf16         ? finch::launch_attend_rows(d, pl.eight, p, s)
-                         : finch::launch_attend_rows_f32(d, p, s);
+    if (e != hipSuccess) break;
+    if (!bf16) {
+      e = finch::launch_attend_rows_f32(d, p, s);
+    } else if (pt == &pl.few) {
+      e = finch::launch_attend_rows16(d, pl.eight, p, s);
+    } else {
+      e = pt == &pl.some ? finch::launch_attend_rows(d, pl.eight, p, s) : finch::launch_attend_tiles(d, pl.eight, p, s);
     }
     if (e == hipSuccess && pt->splits > 1 && !meets) e = finch::launch_attend_join(d, bf16, pt->tile_rows, pt->tile_keys, pt->rows_max, p, s);
   }

@@ -7,6 +7,7 @@
 namespace finch {
 
 hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_rows16(int head_dim, bool eight, const AttendParams& p, hipStream_t s);
 hipError_t launch_attend_tiles(int head_dim, bool eight, const AttendParams& p, hipStream_t s);
 hipError_t launch_attend_rows_f32(int head_dim, const AttendParams& p, hipStream_t s);
 // joins the splits of tiles of `tile_rows` rows and `tile_keys` keys; rows_max: of a problem

@@ -32,6 +32,41 @@ __device__ __forceinline__ int swap_of(int r) {
   return 2 * (r & (D == 128 ? 7 : 3));
 }
 
+// A tile of 32 keys in a wave's registers: 16-byte pieces of K as the kernel's products take them, and of V as they lie in memory.
+template <int D, bool E8>
+struct Tile {
+  static constexpr int kPieces = D / (E8 ? 32 : 16);  // 16-byte pieces a lane has of K, and of V
+  u32x4 k[kPieces], v[kPieces];
+  unsigned ks, vs[kPieces];
+};
+
+template <int D, bool E8>
+__device__ __forceinline__ void load_v(Tile<D, E8>& t, const Part& a, int key0, int shift, int lane) {
+  constexpr int kPer = D / (E8 ? 16 : 8);  // pieces of a row
+#pragma unroll
+  for (int i = 0; i < Tile<D, E8>::kPieces; ++i) {
+    const int id = i * 64 + lane, key = min(key0 + id / kPer, a.n - 1);
+    t.v[i] = as_global<u32x4>(a.v + key * a.row)[id % kPer];
+    if (E8) t.vs[i] = as_global<unsigned char>(a.vs)[key >> shift];
+  }
+}
+
+template <int D, bool E8>
+__device__ __forceinline__ void v_to_lds(const Tile<D, E8>& t, char* lds, int lane) {
+  constexpr int kPer = D / (E8 ? 16 : 8);
+#pragma unroll
+  for (int i = 0; i < Tile<D, E8>::kPieces; ++i) {
+    const int id = i * 64 + lane, r = id / kPer, pc = id % kPer;
+    char* row = lds + r * (2 * D);
+    if (E8) {
+      *reinterpret_cast<bf16x8*>(row + ((2 * pc) ^ swap_of<D>(r)) * 16) = widen(t.v[i][0], t.v[i][1], t.vs[i]);
+      *reinterpret_cast<bf16x8*>(row + ((2 * pc + 1) ^ swap_of<D>(r)) * 16) = widen(t.v[i][2], t.v[i][3], t.vs[i]);
+    } else {
+      *reinterpret_cast<u32x4*>(row + (pc ^ swap_of<D>(r)) * 16) = t.v[i];
+    }
+  }
+}
+
 // The rows' state in a lane: reference (log2 domain), sum of the lane's weights, O^T.
 template <int D>
 struct Rows {

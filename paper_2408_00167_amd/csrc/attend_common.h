@@ -37,6 +37,7 @@ struct AttendParams {
 
 // rows and keys of a tile
 constexpr int kRowsTile = 32, kRowsKeys = 32, kRowsWaves = 4;    // attend_rows
+constexpr int kRows16 = 16;                                      // attend_rows16 (keys and waves as above)
 constexpr int kF32Tile = 16, kF32Keys = 16, kF32Waves = 4;       // attend_rows_f32
 constexpr int kJoinThreads = 256;
 constexpr int kTilesRows = 256, kTilesKeys = 64, kTilesWaves = 8;  // attend_tiles
