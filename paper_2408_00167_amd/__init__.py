@@ -452,7 +452,7 @@ class RowsBatch:
         import torch
         self.n = len(requests)
         self.host = (finch_rows * max(1, self.n))()
-        self.key = None  # (dtype, channels, query heads per KV head or None)
+        self.key = self.suits = None  # (dtype, channels, query heads per KV head or None); the context's it was found to suit
         for i, r in enumerate(requests):
             d = self.host[i]
             parts = {name: r.get(name) for name in ("q", "k", "v")}
@@ -507,7 +507,7 @@ class QuantizeBatch:
         import torch
         self.n = len(problems)
         self.host = (finch_quantization * max(1, self.n))()
-        self.key, self.min_block = None, 1
+        self.key, self.suits, self.min_block = None, None, 1
         for i, pb in enumerate(problems):
             d = self.host[i]
             k, v, ko, vo = (_rows_of(pb[name], 2, name) for name in ("k", "v", "k_out", "v_out"))
@@ -545,7 +545,7 @@ class AttentionBatch:
         import torch
         self.n = len(problems)
         self.host = (finch_attention * max(1, self.n))()
-        self.key, self.min_block, self.planned = None, 1, None
+        self.key, self.suits, self.min_block, self.planned = None, None, 1, None
         for i, pb in enumerate(problems):
             d = self.host[i]
             q, out = _rows_of(pb["q"], 3, "q"), _rows_of(pb["out"], 3, "out")
@@ -601,6 +601,7 @@ class Finch:
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2408_00167_amd needs a GPU: there is no CPU fallback")
         self.device = torch.device(device)
+        self.lib = load_library()
         self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
         with torch.cuda.device(self.index):  # (a context is bound to the device that is current when it is made)
             self.ctx = finch_create(dtype, head_dim, group_size)
@@ -702,10 +703,12 @@ class Finch:
         finch_set_option(self.ctx, FINCH_OPT_SCALE_BLOCK, rows)
         self.scale_block = rows
 
-    def _suits(self, key, what: str) -> None:
+    def _suits(self, batch, what: str) -> None:
         """A batch built of tensors of another type or shape than the context's would be misread."""
+        key = batch.key
         if key is not None and (key[:2] != self.key[:2] or key[2] not in (None, self.key[2])):
             raise ValueError(f"{what}: batch of {key}, context of {self.key}")
+        batch.suits = self.key
 
     def _stream(self, stream):
         """The stream's handle; the current one's without the 3 us that an object for it takes."""
@@ -714,17 +717,23 @@ class Finch:
 
     def rotate(self, batch: RowsBatch, how: Rotary, stream=None):
         """Norm, rotary embedding and placing of projected rows."""
-        self._suits(batch.key, "rotate")
+        if batch.suits is not self.key:
+            self._suits(batch, "rotate")
         if how.norm is not None and (how.norm.dtype, how.norm.shape[0]) != self.key[:2]:
             raise ValueError("rotate: norm weights of another type or size than the context's heads")
-        finch_rotate(self.ctx, how.struct, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
+        st = self.lib.finch_rotate(self.ctx, how.struct, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
+        if st:
+            _check(st, "finch_rotate", self.ctx)
 
     def quantize(self, batch: QuantizeBatch, stream=None):
         """Rows of K and V as e4m3 with one power of two per block of rows."""
-        self._suits(batch.key, "quantize")
+        if batch.suits is not self.key:
+            self._suits(batch, "quantize")
         if batch.min_block > self.scale_block:
             raise ValueError("quantize: too few scales for blocks of this size")
-        finch_quantize(self.ctx, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
+        st = self.lib.finch_quantize(self.ctx, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
+        if st:
+            _check(st, "finch_quantize", self.ctx)
 
     def reserve_attend(self, batch: AttentionBatch) -> int:
         need = finch_attend_workspace_size(self.ctx, batch.host, batch.n)
@@ -734,9 +743,12 @@ class Finch:
 
     def attend(self, batch: AttentionBatch, stream=None):
         """Attention over [cache ; chunk]."""
-        self._suits(batch.key, "attend")
+        if batch.suits is not self.key:
+            self._suits(batch, "attend")
         if batch.min_block > self.scale_block:
             raise ValueError("attend: too few scales for blocks of this size")
         if batch.planned is None or batch.planned[0] is not self or self.ws is None or self.ws.numel() < batch.planned[1]:
             self.reserve_attend(batch)
-        finch_attend(self.ctx, batch.host, batch.dev_ptr, batch.n, self.ws.data_ptr(), self.ws.numel(), self._stream(stream))
+        st = self.lib.finch_attend(self.ctx, batch.host, batch.dev_ptr, batch.n, self.ws.data_ptr(), self.ws.numel(), self._stream(stream))
+        if st:
+            _check(st, "finch_attend", self.ctx)

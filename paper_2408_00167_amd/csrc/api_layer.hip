@@ -63,7 +63,9 @@ bool between_rows(const void* a, const void* b, int64_t n, int64_t row, int64_t 
 }
 
 constexpr int32_t kMostRows = 1 << 24;
-// Most stacked rows of a problem that go to attend_rows.
+// Most stacked rows of a problem that go to attend_rows: its waves read K and V once for 32 rows, attend_tiles once for 256, but with most of
+// its waves idle.  16 requests of 20000 keys, 4 heads on each of 8: 64 rows 279 us there and 328 here, 96 rows 475 and 327; one request of
+// 128 rows on 20000 keys 45 and 32.
 constexpr int kSomeRows = 64;
 constexpr int32_t kMostHeads = 1 << 12;
 
@@ -168,7 +170,9 @@ finch_status plan_attention(const finch_ctx* ctx, const finch_attention* hd, int
     const bool alike = 4 * pt->keys_max * pt->tiles <= 5 * pt->work || pt->tiles < cu;
     if (st == FINCH_OK) st = split(*pt, n, (alike ? 2 : 4) * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
   }
-  if (st == FINCH_OK) st = split(pl.many, n, 2 * cu, 8, cu, ctx->cfg.head_dim, pl.bytes);
+  // Many rows: one workgroup a compute unit, whose eight waves fill it (256 rows of 4 heads on 8 heads' 20000 keys 95 us, 112 with
+  // twice as many).  Where there is a tile of rows for each, no splits: partial results cost more than an uneven end.
+  if (st == FINCH_OK) st = split(pl.many, n, cu, 8, cu, ctx->cfg.head_dim, pl.bytes);
   return st;
 }
 

@@ -59,11 +59,11 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
     float w[4], mx = -kInf;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      w[i] = 4 * part + i < left ? (s0[i] + s1[i]) * prm.scale_log2 : -kInf;
+      w[i] = 4 * part + i < left ? s0[i] + s1[i] : -kInf;
       mx = fmaxf(mx, w[i]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * prm.scale_log2;
     if (__any(mx > ref + kSlack)) {
       const float to = fmaxf(ref, mx), f = ref == -kInf ? 0.f : fast_exp2(ref - to);
       ref = to;
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
     const float at = ref == -kInf ? 0.f : ref;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      w[i] = fast_exp2(w[i] - at);
+      w[i] = fast_exp2(fmaf(w[i], prm.scale_log2, -at));
       sum += w[i];
     }
 #pragma unroll

@@ -32,14 +32,18 @@ __device__ __forceinline__ int swap_in(int r) {
   return V ? swap_of<D>(r) : r & (D / 8 - 1);
 }
 
-template <int D, bool E8>
-__device__ __forceinline__ void fetch(Staged<D>& t, const char* rows, long long row, int n, const unsigned char* exps, int key0, int shift, int tid) {
-  constexpr int kPer = D / (E8 ? 16 : 8);  // pieces of a row
+// MAY: the rows may be e4m3 (`eight`); then all loads are made for either kind, and some of them for nothing: a branch around
+// loads makes the wave wait for them where it ends (96 rows on 10000 keys of 128 heads in 8 bits: 160 us, 255 with one).
+template <int D, bool MAY>
+__device__ __forceinline__ void fetch(Staged<D>& t, bool eight, const char* rows, long long row, int n, const unsigned char* exps, int key0, int shift,
+                                      int tid) {
+  constexpr int kPer = D / 8;  // pieces of a row of bf16; e4m3: half
+  const int per = MAY && eight ? kPer / 2 : kPer, log_per = MAY && eight ? __builtin_ctz(kPer / 2) : __builtin_ctz(kPer);
 #pragma unroll
-  for (int i = 0; i < (E8 ? Staged<D>::kMine8 : Staged<D>::kMine); ++i) {
-    const int id = i * kThreads + tid, key = min(key0 + min(id / kPer, kTilesKeys - 1), n - 1);
-    t.x[i] = as_global<u32x4>(rows + key * row)[id % kPer];
-    if (E8) t.e[i] = as_global<unsigned char>(exps)[key >> shift];
+  for (int i = 0; i < Staged<D>::kMine; ++i) {
+    const int id = i * kThreads + tid, key = min(key0 + min(id >> log_per, kTilesKeys - 1), n - 1);
+    t.x[i] = as_global<u32x4>(rows + key * row)[id & (per - 1)];
+    if (MAY && i < Staged<D>::kMine8) t.e[i] = as_global<unsigned char>(eight ? exps : reinterpret_cast<const unsigned char*>(rows))[eight ? key >> shift : 0];
   }
 }
 
@@ -107,13 +111,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(AttendParams prm) {
   const auto get = [&](Staged<D>& t, int j, bool v) {
     if (j >= all) return;
     const int i = sh.first + j;
-    if (EIGHT && eight && i < sh.cache_tiles) {
-      fetch<D, true>(t, v ? cache.v : cache.k, cache.row, cache.n, v ? cache.vs : cache.ks, i * kTilesKeys, prm.block_shift, tid);
-    } else {
-      const bool in_cache = i < sh.cache_tiles;
-      const Part& a = in_cache ? cache : chunk;
-      fetch<D, false>(t, v ? a.v : a.k, a.row, a.n, nullptr, (in_cache ? i : i - sh.cache_tiles) * kTilesKeys, 0, tid);
-    }
+    const bool in_cache = i < sh.cache_tiles;
+    const Part& a = in_cache ? cache : chunk;
+    fetch<D, EIGHT>(t, EIGHT && eight && in_cache, v ? a.v : a.k, a.row, a.n, v ? cache.vs : cache.ks, (in_cache ? i : i - sh.cache_tiles) * kTilesKeys,
+                    prm.block_shift, tid);
   };
   const auto put_k = [&](int j) {
     if (j >= all) return;
