@@ -335,7 +335,7 @@ typedef struct {
   void* q_out;
   void* k_out;
   void* v_out;
-  const int32_t* pos;  /* device, [n] positions (any int32); NULL: pos0 + t   */
+  const int32_t* pos;  /* device, [n] positions (any int32); NULL: pos0 + t (which has to fit) */
   const int32_t* slot; /* device, [n] rows of k_out and v_out; NULL: row t    */
   int64_t q_row, q_head, k_row, k_head, v_row, v_head;
   int64_t q_out_row, q_out_head, k_out_row, k_out_head, v_out_row, v_out_head;
@@ -433,7 +433,9 @@ typedef struct {
   int32_t causal;         /* 0 or 1                                                     */
 } finch_attention;
 
-/* Bytes of workspace of finch_attend on this batch (0: none is needed). */
+/* Bytes of workspace of finch_attend on this batch (0: none is needed).  The status word of
+ * finch_workspace_status is left alone.  A batch may mix problems of all sizes; what has few rows, some and many goes to a
+ * launch each. */
 finch_status finch_attend_workspace_size(const finch_ctx* ctx, const finch_attention* host_desc, int32_t n_problems,
                                          size_t* bytes);
 finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, const finch_attention* dev_desc,

@@ -397,10 +397,22 @@ class LoopBatch:
         self.dev_first = torch.tensor(first, dtype=torch.int32, device=device)
 
 
-def _upload(host, n: int, struct, device):
+def _upload(batch, struct, device):
+    """The descriptors' copy on the device of the batch's tensors (or `device` where there are none)."""
     import torch
-    raw = bytes(host)[: n * ctypes.sizeof(struct)]
-    return torch.frombuffer(bytearray(raw if raw else b"\0" * 8), dtype=torch.uint8).to(device)
+    raw = bytes(batch.host)[: batch.n * ctypes.sizeof(struct)]
+    batch.dev = torch.frombuffer(bytearray(raw if raw else b"\0" * 8), dtype=torch.uint8).to(device if batch.index is None else batch.index)
+    batch.dev_ptr = batch.dev.data_ptr()
+
+
+def _on_one_gpu(batch, tensors) -> None:
+    """The kernels follow pointers: a tensor in host memory, or on another GPU, must not get that far."""
+    for t in tensors:
+        if t is not None:
+            i = t.get_device()
+            if i < 0 or (batch.index is not None and i != batch.index):
+                raise ValueError("the tensors of a batch must lie on one GPU")
+            batch.index = i
 
 
 def _rows_of(t, dims: int, what: str):
@@ -435,7 +447,8 @@ class Rotary:
     def __init__(self, pairing: int = FINCH_ROPE_HALF, dims: int = 0, freq=None, gain: float = 1.0, q_norm=None, k_norm=None,
                  eps: float = 1e-6):
         import torch
-        self.tensors = (freq, q_norm, k_norm)  # kept alive
+        self.tensors, self.index = (freq, q_norm, k_norm), None  # kept alive; their GPU
+        _on_one_gpu(self, self.tensors)
         self.norm = next((w for w in (q_norm, k_norm) if w is not None), None)
         for w in (q_norm, k_norm):
             if w is not None and (w.dtype != self.norm.dtype or w.dim() != 1 or w.shape != self.norm.shape or not w.is_contiguous()):
@@ -452,9 +465,10 @@ class RowsBatch:
         import torch
         self.n = len(requests)
         self.host = (finch_rows * max(1, self.n))()
-        self.key = self.suits = None  # (dtype, channels, query heads per KV head or None); the context's it was found to suit
+        self.key = self.suits = self.index = None  # (dtype, channels, query heads per KV head or None); the context's it suits; its GPU
         for i, r in enumerate(requests):
             d = self.host[i]
+            _on_one_gpu(self, [r.get(name) for name in ("q", "k", "v", "q_out", "k_out", "v_out", "pos", "slot")])
             parts = {name: r.get(name) for name in ("q", "k", "v")}
             given = {name: t for name, t in parts.items() if t is not None}
             if not given:
@@ -480,7 +494,7 @@ class RowsBatch:
                     raise ValueError("k and v need as many heads, q a multiple of that")
                 group = given["q"].shape[1] // heads[0] if "q" in given else None
             else:
-                d.kv_heads = int(r["kv_heads"])
+                d.kv_heads = int(r.get("kv_heads", 0))
                 if d.kv_heads < 1 or given["q"].shape[1] % d.kv_heads:
                     raise ValueError("q needs a multiple of kv_heads heads")
                 group = given["q"].shape[1] // d.kv_heads
@@ -495,8 +509,7 @@ class RowsBatch:
             if self.key and (key[:2] != self.key[:2] or (self.key[2] is not None and key[2] != self.key[2])):
                 raise ValueError("requests of one batch: types, channels and heads per group must agree")
             self.key = key
-        self.dev = _upload(self.host, self.n, finch_rows, device)
-        self.dev_ptr = self.dev.data_ptr()
+        _upload(self, finch_rows, device)
 
 
 class QuantizeBatch:
@@ -507,9 +520,10 @@ class QuantizeBatch:
         import torch
         self.n = len(problems)
         self.host = (finch_quantization * max(1, self.n))()
-        self.key, self.suits, self.min_block = None, None, 1
+        self.key, self.suits, self.index, self.min_block = None, None, None, 1
         for i, pb in enumerate(problems):
             d = self.host[i]
+            _on_one_gpu(self, [pb[name] for name in ("k", "v", "k_out", "v_out", "k_scale", "v_scale")])
             k, v, ko, vo = (_rows_of(pb[name], 2, name) for name in ("k", "v", "k_out", "v_out"))
             _same([k, v], "k, v")
             if k.shape != v.shape or ko.shape != k.shape or vo.shape != k.shape:
@@ -532,8 +546,10 @@ class QuantizeBatch:
             if self.key not in (None, key):
                 raise ValueError("problems of one batch: types and channels must agree")
             self.key = key
-        self.dev = _upload(self.host, self.n, finch_quantization, device)
-        self.dev_ptr = self.dev.data_ptr()
+        _upload(self, finch_quantization, device)
+
+
+_ATTENTION_TENSORS = ("q", "out", "k_cache", "v_cache", "k_chunk", "v_chunk", "lse", "k_scale", "v_scale", "m_live")
 
 
 class AttentionBatch:
@@ -545,9 +561,10 @@ class AttentionBatch:
         import torch
         self.n = len(problems)
         self.host = (finch_attention * max(1, self.n))()
-        self.key, self.suits, self.min_block, self.planned = None, None, 1, None
+        self.key, self.suits, self.index, self.min_block, self.planned = None, None, None, 1, None
         for i, pb in enumerate(problems):
             d = self.host[i]
+            _on_one_gpu(self, [pb.get(name) for name in _ATTENTION_TENSORS])
             q, out = _rows_of(pb["q"], 3, "q"), _rows_of(pb["out"], 3, "out")
             if q.shape != out.shape or q.dtype != out.dtype:
                 raise ValueError("q and out need one shape and type")
@@ -588,8 +605,7 @@ class AttentionBatch:
             if self.key not in (None, key):
                 raise ValueError("problems of one batch: types, channels and heads per group must agree")
             self.key = key
-        self.dev = _upload(self.host, self.n, finch_attention, device)
-        self.dev_ptr = self.dev.data_ptr()
+        _upload(self, finch_attention, device)
 
 
 class Finch:
@@ -708,6 +724,8 @@ class Finch:
         key = batch.key
         if key is not None and (key[:2] != self.key[:2] or key[2] not in (None, self.key[2])):
             raise ValueError(f"{what}: batch of {key}, context of {self.key}")
+        if batch.index not in (None, self.index):
+            raise ValueError(f"{what}: batch on GPU {batch.index}, context on {self.index}")
         batch.suits = self.key
 
     def _stream(self, stream):
@@ -719,6 +737,8 @@ class Finch:
         """Norm, rotary embedding and placing of projected rows."""
         if batch.suits is not self.key:
             self._suits(batch, "rotate")
+        if how.index not in (None, self.index):
+            raise ValueError("rotate: frequencies or weights on another GPU than the context's")
         if how.norm is not None and (how.norm.dtype, how.norm.shape[0]) != self.key[:2]:
             raise ValueError("rotate: norm weights of another type or size than the context's heads")
         st = self.lib.finch_rotate(self.ctx, how.struct, batch.host, batch.dev_ptr, batch.n, self._stream(stream))

@@ -143,7 +143,7 @@ finch_status split(AttendPlan::Part& pt, int64_t n, int64_t groups, int64_t span
   }
   if (tiles * pt.splits >= (int64_t{1} << 22)) return FINCH_ERR_CAPACITY;
   if (pt.splits > 1) {
-    pt.off_o = off;
+    pt.off_o = off = std::max<size_t>(off, 256);  // (behind the status word that other calls keep there)
     off = align_up(off + static_cast<size_t>(tiles * pt.splits) * pt.tile_rows * head_dim * 4, 256);
     pt.off_ml = off;
     off = align_up(off + static_cast<size_t>(tiles * pt.splits) * pt.tile_rows * 8, 256);

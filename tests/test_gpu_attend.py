@@ -306,3 +306,86 @@ def test_refusals_of_the_binding(context):
     with pytest.raises(F.FinchError) as err:
         F.finch_attend(fin.ctx, batch.host, batch.dev_ptr, 1, fin.ws.data_ptr(), need - 1)
     assert err.value.status == F.FINCH_ERR_WORKSPACE
+
+
+def test_tensors_in_host_memory_are_refused(context):
+    z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    for name in ("q", "out", "k_cache", "v_cache", "k_chunk", "v_chunk"):
+        pb = dict(q=z(1, 4, 128), out=z(1, 4, 128), k_cache=z(3, 128), v_cache=z(3, 128), k_chunk=z(1, 128), v_chunk=z(1, 128))
+        pb[name] = pb[name].cpu()
+        with pytest.raises(ValueError):
+            F.AttentionBatch([pb])
+
+
+def test_the_workspace_keeps_its_status_word():
+    """Partial results stay clear of the word that finch_workspace_status reads."""
+    fin, gen = F.Finch(F.FINCH_BF16, 128, 4), torch.Generator().manual_seed(11)
+    F.finch_set_option(fin.ctx, F.FINCH_OPT_LAYER_GROUP, 2)
+    pbs = [problem(gen, "bf16", 128, 4, n, 9000, n) for n in (1, 10, 40)]
+    batch = F.AttentionBatch(pbs)
+    assert fin.reserve_attend(batch) > 0
+    fin.ws.zero_()
+    fin.attend(batch)
+    assert fin.workspace_status() == 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        fin.attend(batch)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert fin.workspace_status() == 0
+    for pb in pbs:
+        verify(pb, "status word")
+    fin.close()
+
+
+def test_a_captured_call_outlives_its_context():
+    fin, gen = F.Finch(F.FINCH_BF16, 64, 2), torch.Generator().manual_seed(12)
+    pbs = [problem(gen, "bf16", 64, 2, n, 3000, n) for n in (1, 50)]
+    batch = F.AttentionBatch(pbs)
+    fin.reserve_attend(batch)
+    graph, ws = torch.cuda.CUDAGraph(), fin.ws
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        fin.attend(batch)
+    fin.close()
+    for _ in range(3):
+        for pb in pbs:
+            pb["out"].fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        for pb in pbs:
+            verify(pb, "replay without the context")
+    assert ws.numel() > 256
+
+
+def test_two_contexts_on_two_streams_at_once():
+    gen = torch.Generator().manual_seed(13)
+    both = []
+    for _ in range(2):
+        fin = F.Finch(F.FINCH_BF16, 128, 4)
+        pbs = [problem(gen, "bf16", 128, 4, n, 6000, n) for n in (1, 1, 8, 30)]
+        batch = F.AttentionBatch(pbs)
+        fin.reserve_attend(batch)
+        both.append((fin, pbs, batch, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for fin, _, batch, s in both:
+            fin.attend(batch, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for fin, pbs, _, _ in both:
+        for pb in pbs:
+            verify(pb, "beside another context")
+        fin.close()
+
+
+def test_small_and_large_problems_in_one_batch(context):
+    """Generated tokens, a few rows and a whole chunk take three launches; the first token's weights reach far above those of its
+    first tile."""
+    fin, gen = context("bf16", 128, 4), torch.Generator().manual_seed(14)
+    shapes = [(1, 700, 1), (4, 300, 4), (5, 300, 5), (16, 90, 16), (17, 90, 17), (150, 1000, 150), (1, 0, 1)]
+    pbs = [problem(gen, "bf16", 128, 4, *s) for s in shapes]
+    pbs[0]["k_cache"][400] = pbs[0]["q"][0, 1] * 3   # far above the logits before it
+    pbs[5]["k_cache"][500] = pbs[5]["q"][77, 2] * 3
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for s, pb in zip(shapes, pbs):
+        verify(pb, f"mixed {s}")
