@@ -521,28 +521,28 @@ class QuantizeBatch:
         self.n = len(problems)
         self.host = (finch_quantization * max(1, self.n))()
         self.key, self.suits, self.index, self.min_block = None, None, None, 1
+        eight = (torch.uint8, torch.float8_e4m3fn)
         for i, pb in enumerate(problems):
             d = self.host[i]
-            _on_one_gpu(self, [pb[name] for name in ("k", "v", "k_out", "v_out", "k_scale", "v_scale")])
-            k, v, ko, vo = (_rows_of(pb[name], 2, name) for name in ("k", "v", "k_out", "v_out"))
-            _same([k, v], "k, v")
-            if k.shape != v.shape or ko.shape != k.shape or vo.shape != k.shape:
-                raise ValueError("k, v, k_out and v_out need one shape")
-            if k.shape[0] > 1 and (k.stride(0) != v.stride(0) or ko.stride(0) != vo.stride(0)):
-                raise ValueError("k and v, and k_out and v_out, need the same distance between rows")
-            if any(t.dtype not in (torch.uint8, torch.float8_e4m3fn) for t in (ko, vo)):
+            k, v, ko, vo, ks, vs = (pb[name] for name in ("k", "v", "k_out", "v_out", "k_scale", "v_scale"))
+            _on_one_gpu(self, (k, v, ko, vo, ks, vs))
+            shape, dtype = k.shape, k.dtype
+            if len(shape) != 2 or v.shape != shape or ko.shape != shape or vo.shape != shape or v.dtype != dtype:
+                raise ValueError("k, v, k_out and v_out need one shape [n][d], k and v one type")
+            if ko.dtype not in eight or vo.dtype not in eight:
                 raise ValueError("k_out, v_out: want uint8 or float8_e4m3fn")
-            d.n = k.shape[0]
-            d.in_row, d.out_row = k.stride(0), ko.stride(0)
-            if d.n == 1:
-                d.in_row = d.out_row = k.shape[1]
-            for name, t in (("k", k), ("v", v), ("k_out", ko), ("v_out", vo)):
-                setattr(d, name, t.data_ptr() if t.numel() else None)
-            for name in ("k_scale", "v_scale"):
-                setattr(d, name, _flat(pb[name], 1 if d.n else 0, torch.uint8, name))
-                if d.n:
-                    self.min_block = max(self.min_block, -(-d.n // pb[name].numel()))
-            key = (k.dtype, k.shape[1], None)
+            n, width = shape
+            (kr, kc), (vr, vc), (kor, koc), (vor, voc) = k.stride(), v.stride(), ko.stride(), vo.stride()
+            if not kc == vc == koc == voc == 1:
+                raise ValueError("the channels of a head must lie one after the other")
+            if n > 1 and (kr != vr or kor != vor):
+                raise ValueError("k and v, and k_out and v_out, need the same distance between rows")
+            d.n, d.in_row, d.out_row = n, kr if n > 1 else width, kor if n > 1 else width
+            d.k_scale, d.v_scale = _flat(ks, 1 if n else 0, torch.uint8, "k_scale"), _flat(vs, 1 if n else 0, torch.uint8, "v_scale")
+            if n:
+                d.k, d.v, d.k_out, d.v_out = k.data_ptr(), v.data_ptr(), ko.data_ptr(), vo.data_ptr()
+                self.min_block = max(self.min_block, -(-n // min(ks.numel(), vs.numel())))
+            key = (dtype, width, None)
             if self.key not in (None, key):
                 raise ValueError("problems of one batch: types and channels must agree")
             self.key = key
@@ -565,43 +565,46 @@ class AttentionBatch:
         for i, pb in enumerate(problems):
             d = self.host[i]
             _on_one_gpu(self, [pb.get(name) for name in _ATTENTION_TENSORS])
-            q, out = _rows_of(pb["q"], 3, "q"), _rows_of(pb["out"], 3, "out")
-            if q.shape != out.shape or q.dtype != out.dtype:
-                raise ValueError("q and out need one shape and type")
-            d.n_que, group = q.shape[0], q.shape[1]
-            d.q_row, d.q_head, d.out_row, d.out_head = q.stride(0), q.stride(1), out.stride(0), out.stride(1)
-            if d.n_que == 1:
-                d.q_row, d.out_row = q.shape[2], out.shape[2]
-            if group == 1:
-                d.q_head, d.out_head = q.shape[2], out.shape[2]
-            d.q, d.out = (t.data_ptr() if t.numel() else None for t in (q, out))
+            q, out = pb["q"], pb["out"]
+            shape, dtype = q.shape, q.dtype
+            if len(shape) != 3 or out.shape != shape or out.dtype != dtype:
+                raise ValueError("q and out need one shape [n_que][G][d] and type")
+            n_que, group, width = shape
+            (qr, qh, qc), (outr, outh, outc) = q.stride(), out.stride()
+            if qc != 1 or outc != 1:
+                raise ValueError("the channels of a head must lie one after the other")
+            d.n_que = n_que
+            d.q_row, d.out_row = (qr, outr) if n_que > 1 else (width, width)
+            d.q_head, d.out_head = (qh, outh) if group > 1 else (width, width)
+            if n_que:
+                d.q, d.out = q.data_ptr(), out.data_ptr()
             eight = pb.get("k_scale") is not None or pb.get("v_scale") is not None
             for part, count in (("cache", "c"), ("chunk", "m")):
                 k, v = pb.get("k_" + part), pb.get("v_" + part)
-                if (k is None) != (v is None):
-                    raise ValueError(f"k_{part} and v_{part}: both or neither")
-                if k is None:
+                if k is None and v is None:
                     continue
-                _rows_of(k, 2, "k_" + part), _rows_of(v, 2, "v_" + part)
-                if k.shape != v.shape or k.dtype != v.dtype or k.shape[1] != q.shape[2] or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
-                    raise ValueError(f"k_{part} and v_{part}: shapes, types and distances of rows must agree")
-                bytes8 = eight and part == "cache"
-                if k.dtype not in ((torch.uint8, torch.float8_e4m3fn) if bytes8 else (q.dtype,)):
+                if k is None or v is None:
+                    raise ValueError(f"k_{part} and v_{part}: both or neither")
+                rows, ks, vs = k.shape, k.stride(), v.stride()
+                if len(rows) != 2 or v.shape != rows or k.dtype != v.dtype or rows[1] != width or ks[1] != 1 or vs[1] != 1 or (rows[0] > 1 and ks != vs):
+                    raise ValueError(f"k_{part} and v_{part}: shapes [rows][d], types and distances of rows must agree, channels lie one after the other")
+                if k.dtype not in ((torch.uint8, torch.float8_e4m3fn) if eight and part == "cache" else (dtype,)):
                     raise ValueError(f"k_{part}: rows of {k.dtype}")
-                setattr(d, count, k.shape[0])
-                setattr(d, part + "_row", k.stride(0) if k.shape[0] > 1 else k.shape[1])
-                setattr(d, "k_" + part, k.data_ptr() if k.numel() else None)
-                setattr(d, "v_" + part, v.data_ptr() if v.numel() else None)
+                if rows[0]:
+                    setattr(d, count, rows[0])
+                    setattr(d, part + "_row", ks[0] if rows[0] > 1 else width)
+                    setattr(d, "k_" + part, k.data_ptr())
+                    setattr(d, "v_" + part, v.data_ptr())
             if eight:
                 for name in ("k_scale", "v_scale"):
                     if pb.get(name) is None:
                         raise ValueError("k_scale and v_scale: both or neither")
                     setattr(d, name, _flat(pb[name], 1, torch.uint8, name))
                     self.min_block = max(self.min_block, -(-d.c // pb[name].numel()))
-            d.lse = _flat(pb.get("lse"), group * d.n_que, torch.float32, "lse")
+            d.lse = _flat(pb.get("lse"), group * n_que, torch.float32, "lse")
             d.m_live = _flat(pb.get("m_live"), 1, torch.int32, "m_live")
             d.causal = 1 if pb.get("causal", True) else 0
-            key = (q.dtype, q.shape[2], group)
+            key = (dtype, width, group)
             if self.key not in (None, key):
                 raise ValueError("problems of one batch: types, channels and heads per group must agree")
             self.key = key

@@ -377,11 +377,12 @@ def test_two_contexts_on_two_streams_at_once():
         fin.close()
 
 
-def test_small_and_large_problems_in_one_batch(context):
-    """Generated tokens, a few rows and a whole chunk take three launches; the first token's weights reach far above those of its
-    first tile."""
+@pytest.mark.parametrize("large", [(150, 1000, 150), (300, 9000, 300)])
+def test_small_and_large_problems_in_one_batch(context, large):
+    """Generated tokens, a few rows and a whole chunk take three launches, or one where the chunk is most of the work; the first
+    token's weights reach far above those of its first tile."""
     fin, gen = context("bf16", 128, 4), torch.Generator().manual_seed(14)
-    shapes = [(1, 700, 1), (4, 300, 4), (5, 300, 5), (16, 90, 16), (17, 90, 17), (150, 1000, 150), (1, 0, 1)]
+    shapes = [(1, 700, 1), (4, 300, 4), (5, 300, 5), (16, 90, 16), (17, 90, 17), large, (1, 0, 1)]
     pbs = [problem(gen, "bf16", 128, 4, *s) for s in shapes]
     pbs[0]["k_cache"][400] = pbs[0]["q"][0, 1] * 3   # far above the logits before it
     pbs[5]["k_cache"][500] = pbs[5]["q"][77, 2] * 3
