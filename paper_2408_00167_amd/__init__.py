@@ -490,7 +490,7 @@ class RowsBatch:
             group = None
             if heads:
                 d.kv_heads = heads[0]
-                if heads[-1] != heads[0] or ("q" in given and given["q"].shape[1] % heads[0]):
+                if heads[0] < 1 or heads[-1] != heads[0] or ("q" in given and given["q"].shape[1] % heads[0]):
                     raise ValueError("k and v need as many heads, q a multiple of that")
                 group = given["q"].shape[1] // heads[0] if "q" in given else None
             else:

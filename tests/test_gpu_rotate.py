@@ -159,7 +159,8 @@ def test_refusals_of_the_binding():
     good = dict(q=z(3, 4, 128), k=z(3, 2, 128), v=z(3, 2, 128), q_out=z(3, 4, 128), k_out=z(3, 2, 128), v_out=z(3, 2, 128))
     fin.rotate(F.RowsBatch([good]), F.Rotary(F.FINCH_ROPE_OFF))
     for bad in (dict(q=z(2, 4, 128)), dict(k=z(3, 3, 128)), dict(q_out=z(4, 4, 128)), dict(k_out=z(3, 2, 64)), dict(v=z(3, 2, 128, dtype=torch.float32)),
-                dict(pos=z(3, dtype=torch.int64)), dict(slot=z(2, dtype=torch.int32)), dict(q=z(3, 5, 128), q_out=z(3, 5, 128))):
+                dict(pos=z(3, dtype=torch.int64)), dict(slot=z(2, dtype=torch.int32)), dict(q=z(3, 5, 128), q_out=z(3, 5, 128)),
+                dict(k=z(3, 0, 128), k_out=z(3, 0, 128), v=None), dict(k=z(3, 2, 128).cpu())):
         with pytest.raises(ValueError):
             F.RowsBatch([{**good, **bad}])
     with pytest.raises(ValueError):
