@@ -86,7 +86,7 @@ SHAPES = [  # n_que, c, m
     (64, 129, 64), (130, 40, 130), (9, 257, 0), (4, 0, 2), (6, 2, 1)]
 
 
-@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("bf16", 64, 2), ("bf16", 128, 1), ("bf16", 128, 7), ("f32", 64, 1), ("f32", 128, 3)])
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("bf16", 64, 2), ("bf16", 128, 1), ("bf16", 128, 7), ("bf16", 128, 16), ("bf16", 64, 64), ("f32", 64, 1), ("f32", 128, 3)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_ragged_batch_of_all_shapes(context, dtype, d, G, causal):
     fin, gen = context(dtype, d, G), torch.Generator().manual_seed(1)

@@ -179,3 +179,17 @@ def test_reference_knows_its_formats():
     assert R.quantized(x * 1.01, 16)[1] == [1] and R.quantized(x * 0, 16)[1] == [0] and R.quantized(x * 2.0 ** -120, 16)[1] == [-100]
     want = torch.arange(128, dtype=torch.uint8)[:127]
     assert torch.equal(R.e4m3_values(want), want.view(torch.float8_e4m3fn).double())
+
+
+def test_attention_kernels_keep_their_rows_in_registers():
+    """At most four 4-byte values a lane are spilled; a tile of keys, or a row's results, are 16 to 64."""
+    import re
+
+    from tests.test_kernel_registers import kernels
+    seen = 0
+    for name, meta in kernels().items():
+        m = re.search(r"(attend_rows16|attend_rows|attend_tiles|attend_rows_f32|attend_join)ILi(\d+)E", name)
+        if m:
+            seen += 1
+            assert meta[".vgpr_spill_count"] <= 4, f"{name}: {meta['.vgpr_spill_count']} spilled"
+    assert seen == 18  # three bf16 kernels of 2 head sizes, 8-bit caches or not, fp32 of 2, joins of 2 for either type
