@@ -195,15 +195,21 @@ def _check(status: int, where: str, ctx=None):
 
 # ------------------------------------------------------------------ C ABI mirrors
 
+# FINCH_OPT_SCALE_BLOCK of the contexts where it was set: how many scales a call reads or writes goes by it
+_scale_blocks: Dict[int, int] = {}
+
+
 def finch_create(dtype: int, head_dim: int, group_size: int) -> ctypes.c_void_p:
     lib = load_library()
     cfg = finch_config(dtype, head_dim, group_size, 0)
     ctx = ctypes.c_void_p()
     _check(lib.finch_create(ctypes.byref(cfg), ctypes.byref(ctx)), "finch_create")
+    _scale_blocks.pop(ctx.value, None)
     return ctx
 
 
 def finch_destroy(ctx) -> None:
+    _scale_blocks.pop(getattr(ctx, "value", ctx), None)
     _check(load_library().finch_destroy(ctx), "finch_destroy")
 
 
@@ -276,6 +282,8 @@ def finch_profile_read(ctx) -> Dict[str, Dict[str, float]]:
 
 def finch_set_option(ctx, option: int, value: int) -> None:
     _check(load_library().finch_set_option(ctx, option, value), "finch_set_option", ctx)
+    if option == FINCH_OPT_SCALE_BLOCK:
+        _scale_blocks[getattr(ctx, "value", ctx)] = value
 
 
 def finch_set_reposition(ctx, pairing: int = FINCH_ROPE_OFF, order: int = FINCH_ORDER_ASCENDING,
@@ -626,7 +634,11 @@ class Finch:
             self.ctx = finch_create(dtype, head_dim, group_size)
         self.ws = None
         self.key = (torch.bfloat16 if dtype == FINCH_BF16 else torch.float32, head_dim, group_size)
-        self.scale_block = 64
+
+    @property
+    def scale_block(self) -> int:
+        """Rows that share a power of two in 8-bit caches, whichever way the context's option was set."""
+        return 64 if self.ctx is None else _scale_blocks.get(self.ctx.value, 64)
 
     def close(self):
         if self.ctx is not None:
@@ -720,7 +732,6 @@ class Finch:
     def set_scale_block(self, rows: int) -> None:
         """Rows that share a power of two in 8-bit caches (16, 32, 64 or 128)."""
         finch_set_option(self.ctx, FINCH_OPT_SCALE_BLOCK, rows)
-        self.scale_block = rows
 
     def _suits(self, batch, what: str) -> None:
         """A batch built of tensors of another type or shape than the context's would be misread."""
