@@ -630,6 +630,7 @@ class Finch:
         self.device = torch.device(device)
         self.lib = load_library()
         self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        self.device = torch.device(self.device.type, self.index)  # (the workspace's as well, whatever device is current later)
         with torch.cuda.device(self.index):  # (a context is bound to the device that is current when it is made)
             self.ctx = finch_create(dtype, head_dim, group_size)
         self.ws = None

@@ -62,3 +62,19 @@ def test_scales_are_counted_by_the_context_s_block_however_it_was_set(lib):
     fin.close()
     assert fin.scale_block == 64
     other.close()
+
+
+def test_the_workspace_lies_on_the_context_s_gpu_whatever_device_is_current(lib, monkeypatch):
+    """A context is bound to the GPU that is current when it is made; a workspace of another GPU must not reach its kernels."""
+    fin = F.Finch(F.FINCH_BF16, 128, 4)          # GPU 0 is current
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    asked = []
+
+    def empty(*size, device=None, dtype=None):
+        asked.append(torch.device(device))
+        return torch.zeros(*size, dtype=dtype)
+    monkeypatch.setattr(torch, "empty", empty)
+    fin._grow(1000)
+    assert fin.device == torch.device("cuda", 0) and asked == [torch.device("cuda", 0)]
+    second = F.Finch(F.FINCH_BF16, 128, 4)
+    assert second.device == torch.device("cuda", 1) and F.Finch(F.FINCH_BF16, 128, 4, device="cuda:0").index == 0
