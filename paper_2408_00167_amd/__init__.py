@@ -607,8 +607,10 @@ class AttentionBatch:
                 for name in ("k_scale", "v_scale"):
                     if pb.get(name) is None:
                         raise ValueError("k_scale and v_scale: both or neither")
-                    setattr(d, name, _flat(pb[name], 1, torch.uint8, name))
-                    self.min_block = max(self.min_block, -(-d.c // pb[name].numel()))
+                    at = _flat(pb[name], 1 if d.c else 0, torch.uint8, name)
+                    if d.c:
+                        setattr(d, name, at)
+                        self.min_block = max(self.min_block, -(-d.c // pb[name].numel()))
             d.lse = _flat(pb.get("lse"), group * n_que, torch.float32, "lse")
             d.m_live = _flat(pb.get("m_live"), 1, torch.int32, "m_live")
             d.causal = 1 if pb.get("causal", True) else 0

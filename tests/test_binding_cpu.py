@@ -78,3 +78,32 @@ def test_the_workspace_lies_on_the_context_s_gpu_whatever_device_is_current(lib,
     assert fin.device == torch.device("cuda", 0) and asked == [torch.device("cuda", 0)]
     second = F.Finch(F.FINCH_BF16, 128, 4)
     assert second.device == torch.device("cuda", 1) and F.Finch(F.FINCH_BF16, 128, 4, device="cuda:0").index == 0
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """Batches of tensors in host memory, which are described and not uploaded."""
+    monkeypatch.setattr(F, "_on_one_gpu", lambda batch, tensors: setattr(batch, "index", 0))
+    monkeypatch.setattr(F, "_upload", lambda batch, struct, device: setattr(batch, "dev_ptr", 0))
+
+
+def eight_bits(c, scales, rows=1, group=4, d=128):
+    byte = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    half = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    return dict(q=half(rows, group, d), out=half(rows, group, d), k_cache=byte(c, d), v_cache=byte(c, d), k_scale=byte(scales), v_scale=byte(scales),
+                k_chunk=half(rows, d), v_chunk=half(rows, d))
+
+
+def test_an_empty_8_bit_cache_has_no_scales(on_host):
+    """As QuantizeBatch takes it: no rows, no blocks, no scales."""
+    batch = F.AttentionBatch([eight_bits(0, 0), eight_bits(100, 2)])
+    assert [batch.host[i].c for i in range(2)] == [0, 100] and batch.min_block == 50
+    assert not batch.host[0].k_scale and not batch.host[0].v_scale
+    only_one = eight_bits(0, 0)
+    only_one["k_scale"] = torch.zeros(1, dtype=torch.uint8)
+    assert F.AttentionBatch([only_one]).min_block == 1
+    assert not F.AttentionBatch([only_one]).host[0].k_scale
+    with pytest.raises(ValueError):
+        F.AttentionBatch([eight_bits(1, 0)])
+    with pytest.raises(ValueError):
+        F.AttentionBatch([{**eight_bits(0, 0), "v_scale": None}])
