@@ -302,7 +302,8 @@ typedef enum {
    * missing itself, with the same results. */
   FINCH_OPT_LAYER_WAIT_TICKS = 5,
   /* rows that share a power of two in an 8-bit cache (finch_quantize, finch_attend): 16, 32, 64
-   * (default) or 128 */
+   * (default) or 128.  A cache has to be read with the number it was made with: nothing in its
+   * bytes tells the library, and another number gives other values */
   FINCH_OPT_SCALE_BLOCK = 6
 } finch_option;
 typedef enum { FINCH_PATH_AUTO = 0, FINCH_PATH_SEPARATE = 1, FINCH_PATH_OWNER = 3 } finch_path;

@@ -448,6 +448,13 @@ def _same(ts, what: str):
             raise ValueError(f"{what}: types and channels must agree")
 
 
+def _of_block(batch, block) -> None:
+    """The block that a batch's scales are for (None: whichever the context has), and whether they are enough for it."""
+    if block is not None and (block not in (16, 32, 64, 128) or batch.min_block > block):
+        raise ValueError(f"scales for blocks of {block} rows: want 16, 32, 64 or 128, and one for each block")
+    batch.block = block
+
+
 class Rotary:
     """What `Finch.rotate` does to queries and keys: pairing, rotated channels, frequencies ([dims / 2] float64 on the
     device: see finch_rope_frequencies), gain, and the weights of a norm per head ([head_dim])."""
@@ -522,9 +529,9 @@ class RowsBatch:
 
 class QuantizeBatch:
     """Descriptors of `Finch.quantize`: dicts with k, v [n][d], k_out, v_out [n][d] (float8_e4m3fn or uint8), k_scale, v_scale
-    (uint8, one per block of rows)."""
+    (uint8, one per block of rows).  `block`: see AttentionBatch."""
 
-    def __init__(self, problems: Sequence[Dict], device="cuda"):
+    def __init__(self, problems: Sequence[Dict], device="cuda", block: Optional[int] = None):
         import torch
         self.n = len(problems)
         self.host = (finch_quantization * max(1, self.n))()
@@ -554,6 +561,7 @@ class QuantizeBatch:
             if self.key not in (None, key):
                 raise ValueError("problems of one batch: types and channels must agree")
             self.key = key
+        _of_block(self, block)
         _upload(self, finch_quantization, device)
 
 
@@ -563,9 +571,11 @@ _ATTENTION_TENSORS = ("q", "out", "k_cache", "v_cache", "k_chunk", "v_chunk", "l
 class AttentionBatch:
     """Descriptors of `Finch.attend`: dicts with q and out [n_que][G][d], k_cache, v_cache [c][d], k_chunk, v_chunk [m][d] (pairs
     may be None), and optionally lse ([G * n_que] float32), k_scale and v_scale (uint8; the cache rows are then e4m3 bytes, float8_e4m3fn
-    or uint8), m_live (one int32), causal (default True).  The tensors are only read for their device pointers and strides."""
+    or uint8), m_live (one int32), causal (default True).  The tensors are only read for their device pointers and strides.
+    `block`: the rows per power of two that the 8-bit caches were made with; a context that is set to another number refuses the batch.
+    Without it they are read with the context's number, which nothing in the bytes can confirm."""
 
-    def __init__(self, problems: Sequence[Dict], device="cuda"):
+    def __init__(self, problems: Sequence[Dict], device="cuda", block: Optional[int] = None):
         import torch
         self.n = len(problems)
         self.host = (finch_attention * max(1, self.n))()
@@ -618,6 +628,7 @@ class AttentionBatch:
             if self.key not in (None, key):
                 raise ValueError("problems of one batch: types, channels and heads per group must agree")
             self.key = key
+        _of_block(self, block)
         _upload(self, finch_attention, device)
 
 
@@ -745,6 +756,14 @@ class Finch:
             raise ValueError(f"{what}: batch on GPU {batch.index}, context on {self.index}")
         batch.suits = self.key
 
+    def _scales(self, batch, what: str) -> None:
+        """Scales are read and written by the context's block of rows: there have to be enough, and for that block."""
+        block = self.scale_block
+        if batch.min_block > block:
+            raise ValueError(f"{what}: too few scales for blocks of this size")
+        if batch.block not in (None, block):
+            raise ValueError(f"{what}: scales for blocks of {batch.block} rows, context set to {block}")
+
     def _stream(self, stream):
         """The stream's handle; the current one's without the 3 us that an object for it takes."""
         import torch
@@ -766,8 +785,7 @@ class Finch:
         """Rows of K and V as e4m3 with one power of two per block of rows."""
         if batch.suits is not self.key:
             self._suits(batch, "quantize")
-        if batch.min_block > self.scale_block:
-            raise ValueError("quantize: too few scales for blocks of this size")
+        self._scales(batch, "quantize")
         st = self.lib.finch_quantize(self.ctx, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
         if st:
             _check(st, "finch_quantize", self.ctx)
@@ -782,8 +800,7 @@ class Finch:
         """Attention over [cache ; chunk]."""
         if batch.suits is not self.key:
             self._suits(batch, "attend")
-        if batch.min_block > self.scale_block:
-            raise ValueError("attend: too few scales for blocks of this size")
+        self._scales(batch, "attend")
         if batch.planned is None or batch.planned[0] is not self or self.ws is None or self.ws.numel() < batch.planned[1]:
             self.reserve_attend(batch)
         st = self.lib.finch_attend(self.ctx, batch.host, batch.dev_ptr, batch.n, self.ws.data_ptr(), self.ws.numel(), self._stream(stream))

@@ -36,7 +36,7 @@ def lib(monkeypatch):
 
 def batch(fin, min_block):
     """As QuantizeBatch and AttentionBatch look to a call."""
-    return types.SimpleNamespace(host=None, dev_ptr=0, n=1, key=fin.key, suits=None, index=0, min_block=min_block, planned=(fin, 0))
+    return types.SimpleNamespace(host=None, dev_ptr=0, n=1, key=fin.key, suits=None, index=0, min_block=min_block, block=None, planned=(fin, 0))
 
 
 def test_scales_are_counted_by_the_context_s_block_however_it_was_set(lib):
@@ -107,3 +107,33 @@ def test_an_empty_8_bit_cache_has_no_scales(on_host):
         F.AttentionBatch([eight_bits(1, 0)])
     with pytest.raises(ValueError):
         F.AttentionBatch([{**eight_bits(0, 0), "v_scale": None}])
+
+
+def test_a_batch_that_names_its_block_is_not_read_with_another(lib, on_host):
+    """Scales for blocks of 16 rows are more than enough for blocks of 64, and mean other rows."""
+    fin = F.Finch(F.FINCH_BF16, 128, 4)
+    fin.ws = torch.zeros(256, dtype=torch.uint8)
+    cache = eight_bits(100, 7)
+    rows = dict(k=torch.zeros(100, 128, dtype=torch.bfloat16), v=torch.zeros(100, 128, dtype=torch.bfloat16), k_out=cache["k_cache"], v_out=cache["v_cache"],
+                k_scale=cache["k_scale"], v_scale=cache["v_scale"])
+    made, read = F.QuantizeBatch([rows], block=16), F.AttentionBatch([cache], block=16)
+    for context_s in (64, 32, 128):
+        fin.set_scale_block(context_s)
+        lib.calls.clear()
+        with pytest.raises(ValueError):
+            fin.quantize(made)
+        with pytest.raises(ValueError):
+            fin.attend(read)
+        assert lib.calls == []
+    fin.set_scale_block(16)
+    fin.quantize(made, stream=0)
+    fin.attend(read, stream=0)
+    for bad in (0, 8, 48, 256):
+        with pytest.raises(ValueError):
+            F.AttentionBatch([cache], block=bad)
+        with pytest.raises(ValueError):
+            F.QuantizeBatch([rows], block=bad)
+    with pytest.raises(ValueError):  # 100 rows are seven blocks of 16
+        F.AttentionBatch([eight_bits(100, 6)], block=16)
+    with pytest.raises(ValueError):
+        F.QuantizeBatch([{**rows, "v_scale": torch.zeros(6, dtype=torch.uint8)}], block=16)
