@@ -206,6 +206,7 @@ finch_status check_rotation(const finch_ctx* ctx, const finch_rotary* how, const
     if (r.n > kMostRows || r.kv_heads > kMostHeads || (r.slot && r.slots > (1 << 30))) return FINCH_ERR_CAPACITY;
     if (r.n == 0) continue;
     if (!aligned(r.pos, 4) || !aligned(r.slot, 4)) return FINCH_ERR_INVALID_ARG;
+    if (how->pairing != FINCH_ROPE_OFF && !r.pos && r.pos0 > INT32_MAX - (r.n - 1)) return FINCH_ERR_INVALID_ARG;
     const struct {
       const void *in, *out;
       int64_t row, head, out_row, out_head;

@@ -193,3 +193,14 @@ def test_attention_kernels_keep_their_rows_in_registers():
             seen += 1
             assert meta[".vgpr_spill_count"] <= 4, f"{name}: {meta['.vgpr_spill_count']} spilled"
     assert seen == 18  # three bf16 kernels of 2 head sizes, 8-bit caches or not, fp32 of 2, joins of 2 for either type
+
+
+def test_rotate_refuses_positions_past_32_bits():
+    """pos0 + t has to fit, as the header says: t goes to n - 1."""
+    top = (1 << 31) - 1
+    assert check(0, rows(pos0=top - 15), how=rotary()) == F.FINCH_OK
+    assert check(0, rows(pos0=top - 14), how=rotary()) == F.FINCH_ERR_INVALID_ARG
+    assert check(0, rows(pos0=-top - 1), how=rotary()) == F.FINCH_OK
+    # given positions are read instead, and without a rotation none are
+    assert check(0, rows(pos0=top, pos=BASE + 4), how=rotary()) == F.FINCH_OK
+    assert check(0, rows(pos0=top), how=rotary(pairing=F.FINCH_ROPE_OFF, dims=0, freq=None)) == F.FINCH_OK
