@@ -219,6 +219,8 @@ finch_status check_rotation(const finch_ctx* ctx, const finch_rotary* how, const
       if (!p.in) continue;
       if (!p.out || !aligned(p.in, 16) || !aligned(p.out, 16)) return FINCH_ERR_INVALID_ARG;
       if (!stride_ok(p.row, e) || !stride_ok(p.head, e) || !stride_ok(p.out_row, e) || !stride_ok(p.out_head, e)) return FINCH_ERR_INVALID_ARG;
+      // (up to 2^30 slots: stride_ok has 2^24 rows in mind)
+      if (p.slots && r.slots > 0 && p.out_row > (int64_t{1} << 60) / r.slots) return FINCH_ERR_CAPACITY;
       if (!apart(p.slots ? r.slots : r.n, p.out_row, p.heads, p.out_head, d)) return FINCH_ERR_INVALID_ARG;
     }
     if (r.n > n_max) n_max = r.n;

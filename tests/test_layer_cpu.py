@@ -204,3 +204,14 @@ def test_rotate_refuses_positions_past_32_bits():
     # given positions are read instead, and without a rotation none are
     assert check(0, rows(pos0=top, pos=BASE + 4), how=rotary()) == F.FINCH_OK
     assert check(0, rows(pos0=top), how=rotary(pairing=F.FINCH_ROPE_OFF, dims=0, freq=None)) == F.FINCH_OK
+
+
+def test_rotate_strides_times_slots_past_63_bits():
+    """Offsets of 2^30 slots have to stay below 2^60 elements as those of 2^24 tokens do."""
+    far = dict(slot=BASE + 4, slots=1 << 30, v=None, v_out=None)
+    ok = dict(k_out_row=128, k_out_head=1 << 36)
+    assert check(0, rows(**far, **ok), how=rotary()) == F.FINCH_ERR_INVALID_ARG          # 2^30 rows of 128 pass the next head
+    assert check(0, rows(**far, k_out_row=8 * 128, k_out_head=128), how=rotary()) == F.FINCH_OK
+    for row in ((1 << 33), (1 << 35), (1 << 36) - 8):
+        assert check(0, rows(**far, k_out_row=row, k_out_head=128), how=rotary()) == F.FINCH_ERR_CAPACITY, row
+    assert check(0, rows(slot=BASE + 4, slots=1 << 26, v=None, v_out=None, k_out_row=(1 << 36) - 8, k_out_head=128), how=rotary()) == F.FINCH_ERR_CAPACITY
