@@ -646,18 +646,19 @@ class Finch:
         self.device = torch.device(self.device.type, self.index)  # (the workspace's as well, whatever device is current later)
         with torch.cuda.device(self.index):  # (a context is bound to the device that is current when it is made)
             self.ctx = finch_create(dtype, head_dim, group_size)
+        self.handle = self.ctx.value
         self.ws = None
         self.key = (torch.bfloat16 if dtype == FINCH_BF16 else torch.float32, head_dim, group_size)
 
     @property
     def scale_block(self) -> int:
         """Rows that share a power of two in 8-bit caches, whichever way the context's option was set."""
-        return 64 if self.ctx is None else _scale_blocks.get(self.ctx.value, 64)
+        return _scale_blocks.get(self.handle, 64)
 
     def close(self):
         if self.ctx is not None:
             finch_destroy(self.ctx)
-            self.ctx = None
+            self.ctx = self.handle = None
 
     def __del__(self):
         try:
@@ -756,9 +757,8 @@ class Finch:
             raise ValueError(f"{what}: batch on GPU {batch.index}, context on {self.index}")
         batch.suits = self.key
 
-    def _scales(self, batch, what: str) -> None:
+    def _scales(self, batch, block: int, what: str) -> None:
         """Scales are read and written by the context's block of rows: there have to be enough, and for that block."""
-        block = self.scale_block
         if batch.min_block > block:
             raise ValueError(f"{what}: too few scales for blocks of this size")
         if batch.block not in (None, block):
@@ -785,7 +785,9 @@ class Finch:
         """Rows of K and V as e4m3 with one power of two per block of rows."""
         if batch.suits is not self.key:
             self._suits(batch, "quantize")
-        self._scales(batch, "quantize")
+        block = _scale_blocks.get(self.handle, 64)
+        if batch.min_block > block or batch.block is not None:
+            self._scales(batch, block, "quantize")
         st = self.lib.finch_quantize(self.ctx, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
         if st:
             _check(st, "finch_quantize", self.ctx)
@@ -800,7 +802,9 @@ class Finch:
         """Attention over [cache ; chunk]."""
         if batch.suits is not self.key:
             self._suits(batch, "attend")
-        self._scales(batch, "attend")
+        block = _scale_blocks.get(self.handle, 64)
+        if batch.min_block > block or batch.block is not None:
+            self._scales(batch, block, "attend")
         if batch.planned is None or batch.planned[0] is not self or self.ws is None or self.ws.numel() < batch.planned[1]:
             self.reserve_attend(batch)
         st = self.lib.finch_attend(self.ctx, batch.host, batch.dev_ptr, batch.n, self.ws.data_ptr(), self.ws.numel(), self._stream(stream))
