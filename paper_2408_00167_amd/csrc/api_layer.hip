@@ -357,7 +357,8 @@ finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, cons
     p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(d)));
     p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pt->off_o);
     // (a graph outlives its context, and graphs may run side by side: what is captured joins by a launch of its own)
-    const bool meets = pt != &pl.many && pt->splits > 1 && int64_t{n} * pt->row_tiles <= finch::kAttendMeetWords && !finch::being_captured(s);
+    const bool meets = pt != &pl.many && pt->splits > 1 && (pt->splits < finch::kJoinApart || pt->rows_max == 1) &&
+                       int64_t{n} * pt->row_tiles <= finch::kAttendMeetWords && !finch::being_captured(s);
     p.meet = meets ? ctx->attend_meet : nullptr;
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + pt->off_ml);
     if (e != hipSuccess) break;

@@ -40,6 +40,11 @@ constexpr int kRowsTile = 32, kRowsKeys = 32, kRowsWaves = 4;    // attend_rows
 constexpr int kRows16 = 16;                                      // attend_rows16 (keys and waves as above)
 constexpr int kF32Tile = 16, kF32Keys = 16, kF32Waves = 4;       // attend_rows_f32
 constexpr int kJoinThreads = 256;
+// From as many splits on, a launch of its own joins them in any call, a row a workgroup where those are few: 4 rows in 32 splits 10.2 us
+// and 11.3 if the last split to come did it, 32 rows in 64 splits 36 and 56.  Below, the last split does (5 splits: 8.3 us, 9.4 by a
+// launch), or in a captured call a launch that sums in the same order.  A single row is summed in the same order either way, and joined
+// by the last split however many there are (128: 21.3 us, 21.7 by a launch).
+constexpr int kJoinApart = 16;
 constexpr int kTilesRows = 256, kTilesKeys = 64, kTilesWaves = 8;  // attend_tiles
 
 __device__ __forceinline__ finch_attention load_attention(const finch_attention* p) {
@@ -130,16 +135,21 @@ __device__ __forceinline__ bool last_to_come(int32_t* counter, int all, int tid)
 // Joins the splits of rows [first, first + n) of a tile that starts with stacked row r0, by a workgroup of kJoinThreads; at0: where
 // the tile's results begin.  A thread takes four channels of a row in every `groups`-th split, with a running reference, and the
 // groups are joined in LDS: few rows in many splits are read by all threads at once (131000 keys of one request in 125
-// splits took 60 us with the splits of a row behind each other).  The order of the sums depends on sizes alone.
+// splits took 60 us with the splits of a row behind each other).  The order of the sums depends on sizes alone: there are as
+// many groups as for a workgroup that joins `together` >= n rows, of which this one may have a part (HANDED: all).
 template <int D, bool BF16, bool HANDED>
 __device__ __forceinline__ void join_splits(const AttendParams& prm, const Seen& pb, int active, size_t at0, int tile_rows, int r0, int first, int n,
-                                            float* other, int tid) {
-  int per = kJoinThreads / (D / 4);
-  while (per > 1 && per / 2 >= n) per >>= 1;
-  const int items = per * (D / 4), groups = kJoinThreads / items, g = tid / items, it = tid % items, pc = it % (D / 4);
+                                            int together, float* other, int tid) {
+  const auto at_once = [](int rows) {
+    int per = kJoinThreads / (D / 4);
+    while (per > 1 && per / 2 >= rows) per >>= 1;
+    return per;
+  };
+  const int per = at_once(n), items = per * (D / 4), groups = kJoinThreads / ((HANDED ? per : at_once(together)) * (D / 4));
+  const int g = tid / items, it = tid % items, pc = it % (D / 4);
   for (int b = 0; b < n; b += per) {
     const int row = first + b + it / (D / 4), rr = r0 + row;
-    const bool there = b + it / (D / 4) < n;
+    const bool there = b + it / (D / 4) < n && g < groups;
     const float2* ml = prm.part_ml + at0 + row;
     const float* o = prm.part + (at0 + row) * D + 4 * pc;
     float ref = -kInf, total = 0.f;
@@ -147,9 +157,9 @@ __device__ __forceinline__ void join_splits(const AttendParams& prm, const Seen&
     const auto add = [&](float r, float z, f32x4 y) {
       const float to = fmaxf(ref, r), from = to == -kInf ? 0.f : to;
       const float f0 = fast_exp2(ref - from), f1 = fast_exp2(r - from);
-      total = total * f0 + z * f1;
+      total = fmaf(total, f0, z * f1);  // (written out: every kernel that joins has the same roundings)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = sum[e] * f0 + y[e] * f1;
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(sum[e], f0, y[e] * f1);
       ref = to;
     };
     if (there) {

@@ -144,7 +144,8 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
     }
   }
   if (!whole && prm.meet && last_to_come(prm.meet + p * prm.row_tiles + rt, sh.active, tid))
-    join_splits<D, false, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kF32Tile, kF32Tile, r0, 0, min(kF32Tile, pb.R - r0), ex, tid);
+    join_splits<D, false, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kF32Tile, kF32Tile, r0, 0, min(kF32Tile, pb.R - r0),
+                                  min(kF32Tile, pb.R - r0), ex, tid);
 }
 
 hipError_t launch_attend_rows_f32(int head_dim, const AttendParams& p, hipStream_t s) {

@@ -196,7 +196,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
       if (wave == 0 && h == 0) to_others(prm.part_ml + at, f32x2{top, total});
     }
     if (prm.meet && last_to_come(prm.meet + p * prm.row_tiles + rt, sh.active, tid))
-      join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRowsTile, kRowsTile, r0, 0, min(kRowsTile, pb.R - r0), ex, tid);
+      join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRowsTile, kRowsTile, r0, 0, min(kRowsTile, pb.R - r0),
+                                 min(kRowsTile, pb.R - r0), ex, tid);
   }
 }
 
@@ -210,8 +211,9 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join(AttendParams prm, in
   if (!pb.has(prm, r0 + ch * per)) return;
   const Share sh(prm, pb, r0, tile_rows, tile_keys, 0);
   if (sh.active == 1) return;
-  join_splits<D, BF16, false>(prm, pb, sh.active, (static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits * tile_rows, tile_rows, r0, ch * per,
-                              min(per, pb.R - r0 - ch * per), other, threadIdx.x);
+  const int rows = min(tile_rows, pb.R - r0), mine = min(per, rows - ch * per);
+  join_splits<D, BF16, false>(prm, pb, sh.active, (static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits * tile_rows, tile_rows, r0, ch * per, mine,
+                              prm.splits < kJoinApart ? rows : mine, other, threadIdx.x);
 }
 
 hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, hipStream_t s) {
@@ -229,7 +231,7 @@ hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, h
 }
 
 hipError_t launch_attend_join(int head_dim, bool bf16, int tile_rows, int tile_keys, int rows_max, const AttendParams& p, hipStream_t s) {
-  const int per = p.splits >= 16 && static_cast<int64_t>(p.n) * rows_max <= 2048 ? 1 : 8;
+  const int per = p.splits >= kJoinApart && static_cast<int64_t>(p.n) * rows_max <= 2048 ? 1 : 8;
   const int chunks = (std::min(rows_max, tile_rows) + per - 1) / per;  // of a tile of rows
   const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * chunks), block(kJoinThreads);
   if (head_dim == 128 && bf16) {

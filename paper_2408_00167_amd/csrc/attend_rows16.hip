@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, D == 128 ? 2 : 3) void attend_rows
       if (wave == 0 && part == 0) to_others(prm.part_ml + at, f32x2{top, total});
     }
     if (prm.meet && last_to_come(prm.meet + p, sh.active, tid))
-      join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRows16, kRows16, 0, 0, pb.R, ex, tid);
+      join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRows16, kRows16, 0, 0, pb.R, pb.R, ex, tid);
   }
 }
 

@@ -1,0 +1,55 @@
+"""finch_attend in the ways it is called: eagerly and in a replayed graph, many problems of different length in one batch."""
+import pytest
+import torch
+
+import paper_2408_00167_amd as F
+from tests.test_gpu_attend import problem, verify
+
+pytestmark = pytest.mark.gpu
+
+# dtype, channels, heads, 8 bits; (n_que, c, m) of the problems: one workgroup a tile of rows, a few splits, many
+CALLS = [
+    ("bf16", 128, 4, 0, [(1, 1408, 100), (1, 3900, 100), (1, 20, 1), (1, 20000, 3)]),
+    ("bf16", 128, 4, 64, [(1, 30000, 77), (1, 100, 1)]),
+    ("bf16", 128, 4, 0, [(4, 20000, 4), (2, 5000, 2)]),
+    ("bf16", 128, 4, 0, [(8, 20000, 8), (5, 3000, 5), (16, 9000, 16)]),
+    ("bf16", 128, 1, 0, [(1, 40000, 1)]),
+    ("bf16", 64, 8, 0, [(1, 9000, 9), (2, 20000, 9)]),
+    ("bf16", 64, 8, 32, [(4, 20000, 9)]),
+    ("bf16", 64, 2, 0, [(1, 20000, 9)]),
+    ("bf16", 128, 4, 0, [(75, 9000, 75)]),
+    ("f32", 64, 1, 0, [(1, 5000, 1), (256, 48, 256)]),
+    ("f32", 64, 4, 0, [(17, 3000, 17), (3, 9000, 3)]),
+    ("f32", 128, 4, 0, [(1, 5000, 1), (1, 20000, 5)]),
+    ("f32", 128, 2, 0, [(17, 3000, 17), (3, 9000, 3)]),
+]
+
+
+@pytest.mark.parametrize("dtype,d,G,block,shapes", CALLS)
+def test_a_replayed_call_has_the_eager_call_s_bits(dtype, d, G, block, shapes):
+    """The last split to come joins the others in an eager call, a launch of its own in a captured one."""
+    fin, gen = F.Finch(F.FINCH_BF16 if dtype == "bf16" else F.FINCH_F32, d, G), torch.Generator().manual_seed(21)
+    if block:
+        fin.set_scale_block(block)
+    pbs = [problem(gen, dtype, d, G, *s, eight=block) for s in shapes]
+    batch = F.AttentionBatch(pbs)
+    fin.reserve_attend(batch)
+    fin.attend(batch)
+    torch.cuda.synchronize()
+    eager = [(pb["full"].clone(), pb["lse_full"].clone()) for pb in pbs]
+    for s, pb in zip(shapes, pbs):
+        verify(pb, f"eager {dtype} d={d} G={G} {s}", block or 64)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        fin.attend(batch)
+    for replay in range(3):
+        for pb in pbs:
+            pb["out"].fill_(9)
+            pb["lse"].fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        for s, pb, (out, lse) in zip(shapes, pbs, eager):
+            assert torch.equal(pb["full"], out) and torch.equal(pb["lse_full"], lse), f"{dtype} d={d} G={G} {s} replay {replay}"
+        fin.attend(batch)
+        torch.cuda.synchronize()
+    fin.close()
