@@ -436,7 +436,8 @@ typedef struct {
 
 /* Bytes of workspace of finch_attend on this batch (0: none is needed).  The status word of
  * finch_workspace_status is left alone.  A batch may mix problems of all sizes: those of few rows, of some and of many take
- * a launch each, or go along with the last where they are little beside them. */
+ * a launch each, or go along with the last where they are little beside them.  At most 2^24 candidates
+ * and 2^24 stacked rows a problem, and 2^30 pieces of at least 16 rows a batch, else FINCH_ERR_CAPACITY. */
 finch_status finch_attend_workspace_size(const finch_ctx* ctx, const finch_attention* host_desc, int32_t n_problems,
                                          size_t* bytes);
 finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, const finch_attention* dev_desc,

@@ -5,13 +5,15 @@
 #include <cmath>
 
 #include "attend.h"
+#include "attend_plan.h"
 #include "context.h"
 
 namespace {
 
 using finch::aligned;
-using finch::align_up;
+using finch::AttendLaunch;
 using finch::AttendParams;
+using finch::AttendPlan;
 using finch::hip_fail;
 using finch::overlaps;
 
@@ -63,28 +65,7 @@ bool between_rows(const void* a, const void* b, int64_t n, int64_t row, int64_t 
 }
 
 constexpr int32_t kMostRows = 1 << 24;
-// Most stacked rows of a problem that go to attend_rows: its waves read K and V once for 32 rows, attend_tiles once for 256, but with most of
-// its waves idle.  16 requests of 20000 keys, 4 heads on each of 8: 64 rows 279 us there and 328 here, 96 rows 475 and 327; one request of
-// 128 rows on 20000 keys 45 and 32.
-constexpr int kSomeRows = 64;
 constexpr int32_t kMostHeads = 1 << 12;
-
-// How one batch of finch_attend is launched: problems of few rows, of some and of many by kernels of their own.
-struct AttendPlan {
-  struct Part {
-    int tile_rows, tile_keys, rows_lo, rows_hi;
-    int row_tiles = 0, rows_max = 0;  // (no row tiles: nothing to launch)
-    int64_t splits = 1, span = 1;
-    size_t off_o = 0, off_ml = 0;
-    // of its problems: tiles of rows, tiles of keys that these see, most tiles of keys
-    int64_t tiles = 0, work = 0, keys_max = 0;
-  };
-  Part few = {finch::kRows16, finch::kRowsKeys, 1, finch::kRows16};
-  Part some = {finch::kRowsTile, finch::kRowsKeys, finch::kRows16 + 1, kSomeRows};
-  Part many = {finch::kTilesRows, finch::kTilesKeys, kSomeRows + 1, INT32_MAX};
-  bool eight = false;
-  size_t bytes = 0;
-};
 
 finch_status check_attention(const finch_ctx* ctx, const finch_attention& a) {
   const int e = elem_bytes(ctx), G = ctx->cfg.group_size;
@@ -113,79 +94,30 @@ finch_status check_attention(const finch_ctx* ctx, const finch_attention& a) {
   return FINCH_OK;
 }
 
-void count(AttendPlan::Part& pt, const finch_attention& a, int64_t rows) {
-  const int64_t tiles = (rows + pt.tile_rows - 1) / pt.tile_rows, cache = (a.c + pt.tile_keys - 1) / pt.tile_keys;
-  const int64_t keys = cache + (a.m + pt.tile_keys - 1) / pt.tile_keys;
-  if (tiles > pt.row_tiles) pt.row_tiles = static_cast<int>(tiles);
-  if (keys > pt.keys_max) pt.keys_max = keys;
-  if (rows > pt.rows_max) pt.rows_max = static_cast<int>(rows);
-  pt.tiles += tiles;
-  // (causal rows of the chunk itself see half of themselves on average)
-  const int64_t own = a.causal ? std::min(a.n_que, a.m) / 2 / pt.tile_keys : 0;
-  pt.work += tiles * (keys - own);
-}
-
-// Splits: where tiles of rows are too few for the chip, the keys each sees are dealt out to several workgroups of `span` tiles at
-// least, so that there are about `groups` workgroups.
-finch_status split(AttendPlan::Part& pt, int64_t n, int64_t groups, int64_t span_min, int64_t enough, int head_dim, size_t& off) {
-  const int64_t tiles = n * pt.row_tiles, part = int64_t{pt.tile_rows} * (head_dim + 2) * 4;
-  if (tiles == 0) return FINCH_OK;
-  // (a join takes its time with the number of splits, so that it is shortest with the square root of all tiles)
-  span_min = std::max(span_min, static_cast<int64_t>(std::sqrt(0.5 * static_cast<double>(pt.keys_max))));
-  pt.span = std::max((pt.work + groups - 1) / groups, span_min);
-  if (pt.tiles >= enough) pt.span = std::max<int64_t>(pt.keys_max, 1);
-  // (partial results of at most 64 MiB and 2^15 tiles of rows)
-  const int64_t most = std::max<int64_t>(1, std::min((int64_t{64} << 20) / part, int64_t{1} << 15) / tiles);
-  pt.splits = std::max<int64_t>(1, (pt.keys_max + pt.span - 1) / pt.span);
-  if (pt.splits > most) {
-    pt.splits = most;
-    pt.span = (pt.keys_max + most - 1) / most;
-  }
-  if (tiles * pt.splits >= (int64_t{1} << 22)) return FINCH_ERR_CAPACITY;
-  if (pt.splits > 1) {
-    pt.off_o = off = std::max<size_t>(off, 256);  // (behind the status word that other calls keep there)
-    off = align_up(off + static_cast<size_t>(tiles * pt.splits) * pt.tile_rows * head_dim * 4, 256);
-    pt.off_ml = off;
-    off = align_up(off + static_cast<size_t>(tiles * pt.splits) * pt.tile_rows * 8, 256);
-  }
-  return FINCH_OK;
-}
-
 finch_status plan_attention(const finch_ctx* ctx, const finch_attention* hd, int32_t n, AttendPlan& pl) {
   const bool bf16 = ctx->cfg.dtype == FINCH_BF16;
-  const int G = ctx->cfg.group_size, cu = ctx->n_cu > 0 ? ctx->n_cu : 256;
-  if (!bf16) pl.some = {finch::kF32Tile, finch::kF32Keys, 1, INT32_MAX};
+  const int G = ctx->cfg.group_size, d = ctx->cfg.head_dim, cu = ctx->n_cu > 0 ? ctx->n_cu : 256;
   for (int32_t i = 0; i < n; ++i) {
     const finch_status st = check_attention(ctx, hd[i]);
     if (st != FINCH_OK) return st;
     if (hd[i].k_scale) pl.eight = true;
     const int64_t rows = int64_t{hd[i].n_que} * G;
-    if (rows > 0) count(!bf16 ? pl.some : rows <= pl.few.rows_hi ? pl.few : rows <= pl.some.rows_hi ? pl.some : pl.many, hd[i], rows);
+    if (rows > 0) (!bf16 ? pl.some : rows <= pl.few.rows_hi ? pl.few : rows <= pl.some.rows_hi ? pl.some : pl.many).add(hd[i], i, rows);
   }
-  // What is little beside the problems of many rows goes along with them: a launch of its own would take longer (five packed prompts on
-  // 32 heads, one of them of 58 rows: 110 us with one, 107 without).
-  const auto little = [&](const AttendPlan::Part& pt) { return pl.many.row_tiles > 0 && 8 * pt.work <= pl.many.work; };
-  if (little(pl.some)) {
-    const int lo = little(pl.few) ? pl.few.rows_lo : pl.some.rows_lo, hi = pl.some.rows_hi;
-    for (int32_t i = 0; i < n; ++i) {
-      const int64_t rows = int64_t{hd[i].n_que} * G;
-      if (rows >= lo && rows <= hi) count(pl.many, hd[i], rows);
-    }
-    pl.many.rows_lo = lo;
-    pl.some.row_tiles = 0;
-    if (lo == pl.few.rows_lo) pl.few.row_tiles = 0;
+  // What is little beside the problems of many rows, and no longer than their workgroups, goes along with them: a launch of its own would
+  // take longer (five packed prompts on 32 heads, one of them of 58 rows: 114 us with one, 109 without).
+  const auto little = [&](const AttendLaunch& l) { return pl.many.tiles > 0 && 8 * l.work <= pl.many.work && 8 * l.keys_max * cu <= pl.many.work; };
+  if (pl.few.tiles + pl.some.tiles > 0 && little(pl.some)) {
+    const int lo = little(pl.few) ? pl.few.rows_lo : pl.some.rows_lo;
+    pl.many = AttendLaunch(finch::kTilesRows, finch::kTilesKeys, lo, INT32_MAX);
+    for (int32_t i = 0; i < n; ++i)
+      if (int64_t{hd[i].n_que} * G >= lo) pl.many.add(hd[i], i, int64_t{hd[i].n_que} * G);
+    pl.some.tiles = 0;
+    if (lo == pl.few.rows_lo) pl.few.tiles = 0;
   }
-  finch_status st = FINCH_OK;
-  for (AttendPlan::Part* pt : {&pl.few, &pl.some}) {
-    // Two workgroups a compute unit are on the chip at once, and as many are enough where they are alike or few (one request,
-    // 131000 keys in 8 bits: 60 us, 73 with twice as many; 512 problems of 2000 keys 92 and 108 us); problems of different
-    // length level out with twice as many (512 of 64 to 8192 keys 224 us, 236 with half).
-    const bool alike = 4 * pt->keys_max * pt->tiles <= 5 * pt->work || pt->tiles < cu;
-    if (st == FINCH_OK) st = split(*pt, n, (alike ? 2 : 4) * cu, 4, INT64_MAX, ctx->cfg.head_dim, pl.bytes);
-  }
-  // Many rows: one workgroup a compute unit, whose eight waves fill it (256 rows of 4 heads on 8 heads' 20000 keys 95 us, 112 with
-  // twice as many).  Where there is a tile of rows for each, no splits: partial results cost more than an uneven end.
-  if (st == FINCH_OK) st = split(pl.many, n, cu, 8, cu, ctx->cfg.head_dim, pl.bytes);
+  finch_status st = pl.few.deal(false, cu, d, G, pl.bytes);
+  if (st == FINCH_OK) st = pl.some.deal(false, cu, d, G, pl.bytes);
+  if (st == FINCH_OK) st = pl.many.deal(true, cu, d, G, pl.bytes);
   return st;
 }
 
@@ -322,7 +254,7 @@ finch_status finch_quantize(finch_ctx* ctx, const finch_quantization* host_desc,
 
 finch_status finch_attend_workspace_size(const finch_ctx* ctx, const finch_attention* host_desc, int32_t n, size_t* bytes) {
   if (!ctx || !bytes || n < 0 || (n > 0 && !host_desc)) return FINCH_ERR_INVALID_ARG;
-  AttendPlan pl;
+  AttendPlan pl(ctx->cfg.dtype == FINCH_BF16);
   const finch_status st = plan_attention(ctx, host_desc, n, pl);
   *bytes = st == FINCH_OK ? pl.bytes : 0;
   return st;
@@ -332,44 +264,46 @@ finch_status finch_attend(finch_ctx* ctx, const finch_attention* host_desc, cons
                           size_t ws_bytes, void* stream) {
   finch_status st = check_batch(ctx, host_desc, dev_desc, n);
   if (st != FINCH_OK) return st;
-  AttendPlan pl;
+  AttendPlan pl(ctx->cfg.dtype == FINCH_BF16);
   if ((st = plan_attention(ctx, host_desc, n, pl)) != FINCH_OK) return st;
   if (pl.bytes > 0 && (!ws || !aligned(ws, 256) || ws_bytes < pl.bytes)) return FINCH_ERR_WORKSPACE;
-  if (pl.few.row_tiles == 0 && pl.some.row_tiles == 0 && pl.many.row_tiles == 0) return FINCH_OK;
+  if (pl.few.tiles == 0 && pl.some.tiles == 0 && pl.many.tiles == 0) return FINCH_OK;
   const OnDevice on(ctx);
   if (on.e != hipSuccess) return done(ctx, on.e);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = ctx->cfg.dtype == FINCH_BF16;
   const int d = ctx->cfg.head_dim;
   hipError_t e = hipSuccess;
-  for (const AttendPlan::Part* pt : {&pl.many, &pl.some, &pl.few}) {
-    if (pt->row_tiles == 0) continue;
+  for (const AttendLaunch* l : {&pl.many, &pl.some, &pl.few}) {
+    if (l->tiles == 0) continue;
     AttendParams p;
     p.descs = dev_desc;
-    p.n = n;
     p.group = ctx->cfg.group_size;
-    p.rows_lo = pt->rows_lo;
-    p.rows_hi = pt->rows_hi;
-    p.row_tiles = pt->row_tiles;
-    p.splits = static_cast<int32_t>(pt->splits);
-    p.span = static_cast<int32_t>(pt->span);
+    l->table(p);
     p.block_shift = __builtin_ctz(static_cast<unsigned>(ctx->scale_block));
     p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(d)));
-    p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pt->off_o);
+    p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + l->off_o);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + l->off_ml);
     // (a graph outlives its context, and graphs may run side by side: what is captured joins by a launch of its own)
-    const bool meets = pt != &pl.many && pt->splits > 1 && (pt->splits < finch::kJoinApart || pt->rows_max == 1) &&
-                       int64_t{n} * pt->row_tiles <= finch::kAttendMeetWords && !finch::being_captured(s);
+    const bool meets = l != &pl.many && l->slots > 0 && (l->most_splits < finch::kJoinApart || l->rows_max == 1) && !finch::being_captured(s);
     p.meet = meets ? ctx->attend_meet : nullptr;
-    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + pt->off_ml);
-    if (e != hipSuccess) break;
-    if (!bf16) {
-      e = finch::launch_attend_rows_f32(d, p, s);
-    } else if (pt == &pl.few) {
-      e = finch::launch_attend_rows16(d, pl.eight, p, s);
-    } else {
-      e = pt == &pl.some ? finch::launch_attend_rows(d, pl.eight, p, s) : finch::launch_attend_tiles(d, pl.eight, p, s);
+    for (int64_t at = 0; at < l->workgroups && e == hipSuccess; at += finch::kLaunchGrid) {
+      const int some = static_cast<int>(std::min<int64_t>(finch::kLaunchGrid, l->workgroups - at));
+      p.base = static_cast<int32_t>(at);
+      if (!bf16) {
+        e = finch::launch_attend_rows_f32(d, p, some, s);
+      } else if (l == &pl.few) {
+        e = finch::launch_attend_rows16(d, pl.eight, p, some, s);
+      } else {
+        e = l == &pl.some ? finch::launch_attend_rows(d, pl.eight, p, some, s) : finch::launch_attend_tiles(d, pl.eight, p, some, s);
+      }
     }
-    if (e == hipSuccess && pt->splits > 1 && !meets) e = finch::launch_attend_join(d, bf16, pt->tile_rows, pt->tile_keys, pt->rows_max, p, s);
+    if (e == hipSuccess && l->slots > 0 && !meets) {
+      int problems = 0;
+      const int tiles = l->join_table(p, problems);
+      e = finch::launch_attend_join(d, bf16, l->tile_rows, l->tile_keys, l->rows_max, problems, tiles, p, s);
+    }
+    if (e != hipSuccess) break;
   }
   return done(ctx, e);
 }
@@ -383,10 +317,37 @@ finch_status finch_debug_layer_check(const finch_config* cfg, int32_t scale_bloc
   tmp.cfg = *cfg;
   tmp.scale_block = scale_block;
   int32_t n_max = 0;
-  AttendPlan pl;
+  AttendPlan pl(cfg->dtype == FINCH_BF16);
   if (call == 0) return check_rotation(&tmp, how, static_cast<const finch_rows*>(desc), n, n_max);
   if (call == 1) return check_quantization(&tmp, static_cast<const finch_quantization*>(desc), n, n_max);
   return plan_attention(&tmp, static_cast<const finch_attention*>(desc), n, pl);
+}
+
+// (Likewise.)  How finch_attend launches a batch on a chip of `cu` compute units.  kernel: 0 few rows, 1 some (or fp32), 2 many.
+// said: workgroups, tiles of keys of a split at most, most splits, slots of partial results, tiles of rows that are joined, bytes of
+// workspace, fewest and most stacked rows of its problems.  pieces, or NULL: [workgroups][5], of each its problem, tile of rows, split, splits and its tile's first slot.
+finch_status finch_debug_attend_plan(const finch_config* cfg, int32_t cu, const finch_attention* desc, int32_t n, int32_t kernel, int64_t* said,
+                                     int32_t* pieces) {
+  if (!cfg || n < 0 || (n > 0 && !desc) || kernel < 0 || kernel > 2 || !said) return FINCH_ERR_INVALID_ARG;
+  finch_ctx tmp = {};
+  tmp.cfg = *cfg;
+  tmp.scale_block = 64;
+  tmp.n_cu = cu;
+  AttendPlan pl(cfg->dtype == FINCH_BF16);
+  const finch_status st = plan_attention(&tmp, desc, n, pl);
+  if (st != FINCH_OK) return st;
+  const AttendLaunch& l = kernel == 0 ? pl.few : kernel == 1 ? pl.some : pl.many;
+  AttendParams p;
+  int problems = 0;
+  const int64_t got[8] = {l.workgroups, l.span, l.most_splits, l.slots, l.join_table(p, problems), static_cast<int64_t>(pl.bytes), l.rows_lo, l.rows_hi};
+  std::copy(got, got + 8, said);
+  l.table(p);
+  for (int64_t w = 0; pieces && w < l.workgroups; ++w) {
+    const finch::AttendPiece x = finch::piece_of(p, static_cast<int>(w));
+    const int32_t five[5] = {x.p, x.rt, x.split, x.splits, x.slot};
+    std::copy(five, five + 5, pieces + 5 * w);
+  }
+  return FINCH_OK;
 }
 
 }  // extern "C"

@@ -6,8 +6,11 @@
 //
 // Keys.  A tile is KT consecutive rows of the cache or of the chunk, never of both; tiles of the
 // cache come first.  Rows past a part's last one are read as that one again and masked.  The
-// tiles a tile of rows sees are dealt out to `splits` workgroups, `span` tiles each at least;
+// tiles a tile of rows sees are dealt out to `splits` workgroups, `span` tiles each at most;
 // what they have is joined by attend_join.
+//
+// Workgroups.  A launch has as many as there are pieces of work: its problems lie in runs of neighbours in the batch that
+// have as many tiles of rows and of keys, and each run's workgroups follow those of the run before.
 #pragma once
 
 #include "score_common.h"
@@ -20,20 +23,74 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
+// Tiles of rows top, top - 1, .. (`levels` of them) of `count` problems from `problem` on, each by `splits` workgroups (some of a
+// run that stands for unlike problems have nothing to do).
+struct AttendRun {
+  int32_t problem, count, top, levels;
+  int32_t splits;
+  int32_t slot;         // where the run's partial results begin (splits > 1)
+};
+// (The table goes along as kernel arguments: with 64, 2 KB in all, a single token's call that is waited for took 21 to 33 us,
+// 21 with 32, and batches of 64 and 128 tokens 222 and 233 us in place of 216 and 232.)
+constexpr int kMostRuns = 32;
+
 struct AttendParams {
   const finch_attention* descs;
-  int32_t n;            // problems
   int32_t group;        // G
   int32_t rows_lo, rows_hi;  // problems with as many stacked rows are this launch's
-  int32_t row_tiles;    // of the problem with the most rows
-  int32_t splits;       // most workgroups on one tile of rows
-  int32_t span;         // tiles of keys a split has at least (but the last)
+  int32_t most_splits;  // of a run
+  int32_t span;         // tiles of keys a split has at most
   int32_t block_shift;  // log2 of the rows per power of two of an 8-bit cache
   float scale_log2;     // log2(e) / sqrt(d_k)
-  float* part;          // [n][row_tiles][splits][rows of a tile][D] sums of weighted values ...
-  int32_t* meet;        // a counter per problem and tile of rows, at zero between launches: the last split to come joins them; null: attend_join
-  float2* part_ml;      // ... and [n][row_tiles][splits][rows of a tile] (reference, sum of weights)
+  float* part;          // [slots][rows of a tile][D] sums of weighted values: `splits` slots one after the other for each tile of rows ...
+  float2* part_ml;      // ... and [slots][rows of a tile] (reference, sum of weights)
+  int32_t* meet;        // a counter per slot, at zero between launches: the last split to come joins a tile's; null: attend_join
+  int32_t base;         // number of the launch's first workgroup
+  int32_t runs;
+  AttendRun one;             // the only run, beside what a workgroup reads first anyway; or, with more of them:
+  int32_t start[kMostRuns];  // a run's first workgroup
+  AttendRun run[kMostRuns];
 };
+
+// The run of workgroup w, whose number in it w becomes.
+__host__ __device__ __forceinline__ AttendRun run_of(const AttendParams& prm, int& w) {
+  AttendRun r = prm.one;
+#ifdef __HIP_DEVICE_COMPILE__
+  // (now and together: left to itself the compiler fetches each where it is used, one round trip after the other)
+  asm volatile("" : "+s"(r.problem), "+s"(r.count), "+s"(r.top), "+s"(r.levels), "+s"(r.splits), "+s"(r.slot) : "s"(prm.descs), "s"(prm.runs));
+#endif
+  if (prm.runs > 1) {
+    int e = 0;
+#ifdef __HIP_DEVICE_COMPILE__
+    static_assert(kMostRuns <= 64, "a run a lane");
+    const int lane = threadIdx.x & 63;
+    e = uni(static_cast<int>(__popcll(__ballot(lane < prm.runs && prm.start[lane] <= w))) - 1);
+#else
+    while (e + 1 < prm.runs && prm.start[e + 1] <= w) ++e;
+#endif
+    r = prm.run[e];
+    w -= prm.start[e];
+  }
+  return r;
+}
+
+// What workgroup w has.
+struct AttendPiece {
+  int p, rt;            // problem, tile of rows
+  int split, splits;
+  int slot;             // of the tile's first split
+};
+__host__ __device__ __forceinline__ AttendPiece piece_of(const AttendParams& prm, int w) {
+  const AttendRun r = run_of(prm, w);
+  const int tiles = r.count * r.levels, split = w / tiles, t = w - split * tiles, level = t / r.count;
+  AttendPiece x;
+  x.p = r.problem + t - level * r.count;
+  x.rt = r.top - level;
+  x.split = split;
+  x.splits = r.splits;
+  x.slot = r.slot + t * r.splits;
+  return x;
+}
 
 // rows and keys of a tile
 constexpr int kRowsTile = 32, kRowsKeys = 32, kRowsWaves = 4;    // attend_rows
@@ -84,11 +141,11 @@ struct Share {
   int cache_tiles, tiles;  // all that the rows see
   int active;              // splits with any
   int first, last;         // this split's
-  __device__ __forceinline__ Share(const AttendParams& prm, const Seen& pb, int r0, int rows, int kt, int s) {
+  __device__ __forceinline__ Share(const AttendParams& prm, const Seen& pb, int r0, int rows, int kt, int s, int splits) {
     const int lim = pb.limit(min(r0 + rows, pb.R) - 1);
     cache_tiles = (min(lim, pb.d.c) + kt - 1) / kt;
     tiles = cache_tiles + (max(lim - pb.d.c, 0) + kt - 1) / kt;
-    active = max(1, min(prm.splits, (tiles + prm.span - 1) / prm.span));
+    active = max(1, min(splits, (tiles + prm.span - 1) / prm.span));
     const int per = (tiles + active - 1) / active;
     first = min(s * per, tiles);
     last = min(first + per, tiles);

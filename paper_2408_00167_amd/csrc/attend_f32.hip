@@ -12,11 +12,12 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
   __shared__ float ex[kF32Waves * 3 * kQuarter * 64];
   static_assert(kF32Waves * 3 * kQuarter * 64 >= kJoinThreads * 6, "join_splits");
   __shared__ float ml[2][kF32Waves][kF32Tile];
-  const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = rest % prm.row_tiles, split = rest / prm.row_tiles;
-  const Seen pb(prm, p);
-  const int r0 = rt * kF32Tile;
+  const AttendPiece piece = piece_of(prm, prm.base + blockIdx.x);
+  const int split = piece.split;
+  const Seen pb(prm, piece.p);
+  const int r0 = piece.rt * kF32Tile;
   if (!pb.has(prm, r0)) return;
-  const Share sh(prm, pb, r0, kF32Tile, kF32Keys, split);
+  const Share sh(prm, pb, r0, kF32Tile, kF32Keys, split, piece.splits);
   if (split >= sh.active) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), row = lane & 15, part = lane >> 4;
   const int rr = min(r0 + row, pb.R - 1), tok = rr / pb.group, head = rr % pb.group;
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
     for (int w = 0; w < 3; ++w) own[x] += from[w * kQuarter * 64];
   }
   const bool there = r0 + row < pb.R, whole = sh.active == 1;
-  const size_t at = ((static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits + split) * kF32Tile + row;
+  const size_t at = static_cast<size_t>(piece.slot + split) * kF32Tile + row;
   if (there) {
     const float inv = total > 0.f ? 1.f / total : 0.f;
     float* to = static_cast<float*>(pb.d.out) + tok * pb.d.out_row + head * pb.d.out_head;
@@ -143,13 +144,13 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_rows_f32(AttendParams p
       }
     }
   }
-  if (!whole && prm.meet && last_to_come(prm.meet + p * prm.row_tiles + rt, sh.active, tid))
+  if (!whole && prm.meet && last_to_come(prm.meet + piece.slot, sh.active, tid))
     join_splits<D, false, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kF32Tile, kF32Tile, r0, 0, min(kF32Tile, pb.R - r0),
                                   min(kF32Tile, pb.R - r0), ex, tid);
 }
 
-hipError_t launch_attend_rows_f32(int head_dim, const AttendParams& p, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * p.splits), block(64 * kF32Waves);
+hipError_t launch_attend_rows_f32(int head_dim, const AttendParams& p, int workgroups, hipStream_t s) {
+  const dim3 grid(workgroups), block(64 * kF32Waves);
   if (head_dim == 128) {
     hipLaunchKernelGGL((attend_rows_f32<128>), grid, block, 0, s, p);
   } else {

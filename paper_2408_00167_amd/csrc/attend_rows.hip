@@ -96,11 +96,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
   __shared__ __align__(16) char lds[kRowsWaves * 3 * kQuarter * 64 * 4];
   __shared__ float ml[2][kRowsWaves][kRowsTile];
   static_assert(sizeof(lds) >= kRowsWaves * kRowsKeys * D * 2, "V tiles of all waves");
-  const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = rest % prm.row_tiles, split = rest / prm.row_tiles;
-  const Seen pb(prm, p);
-  const int r0 = rt * kRowsTile;
+  const AttendPiece piece = piece_of(prm, prm.base + blockIdx.x);
+  const int split = piece.split;
+  const Seen pb(prm, piece.p);
+  const int r0 = piece.rt * kRowsTile;
   if (!pb.has(prm, r0)) return;
-  const Share sh(prm, pb, r0, kRowsTile, kRowsKeys, split);
+  const Share sh(prm, pb, r0, kRowsTile, kRowsKeys, split, piece.splits);
   if (split >= sh.active) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), h = lane >> 5;
   const int row = lane & 31, rr = min(r0 + row, pb.R - 1), tok = rr / pb.group, head = rr % pb.group;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
     if (pb.d.lse && wave == 0 && h == 0)
       as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
   } else {
-    const size_t at = ((static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits + split) * kRowsTile + row;
+    const size_t at = static_cast<size_t>(piece.slot + split) * kRowsTile + row;
     if (there) {
 #pragma unroll
       for (int x = 0; x < kQuarter; x += 4) {
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
       }
       if (wave == 0 && h == 0) to_others(prm.part_ml + at, f32x2{top, total});
     }
-    if (prm.meet && last_to_come(prm.meet + p * prm.row_tiles + rt, sh.active, tid))
+    if (prm.meet && last_to_come(prm.meet + piece.slot, sh.active, tid))
       join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRowsTile, kRowsTile, r0, 0, min(kRowsTile, pb.R - r0),
                                  min(kRowsTile, pb.R - r0), ex, tid);
   }
@@ -203,21 +204,25 @@ __global__ __launch_bounds__(64 * kRowsWaves, 2) void attend_rows(AttendParams p
 
 // Joins the splits of `per` rows of a tile of rows (see join_splits).
 template <int D, bool BF16>
-__global__ __launch_bounds__(kJoinThreads) void attend_join(AttendParams prm, int tile_rows, int tile_keys, int per, int chunks) {
+__global__ __launch_bounds__(kJoinThreads) void attend_join(int tile_rows, int tile_keys, int per, int chunks, AttendParams prm) {
   __shared__ float other[kJoinThreads * 6];
-  const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, ch = rest % chunks, rt = rest / chunks;
-  const Seen pb(prm, p);
-  const int r0 = rt * tile_rows;
+  // (a run here has `chunks` workgroups for each tile of rows, problems fastest, and last the last tiles of rows, which may have few: 300 rows
+  // of 4 problems on 9000 keys 31.3 us in all, 32.5 the other way round)
+  int w = blockIdx.x;
+  const AttendRun r = run_of(prm, w);
+  const int back = w / (r.count * chunks), at = w - back * r.count * chunks, ch = at / r.count, i = at - ch * r.count, level = r.levels - 1 - back;
+  const Seen pb(prm, r.problem + i);
+  const int r0 = (r.top - level) * tile_rows;
   if (!pb.has(prm, r0 + ch * per)) return;
-  const Share sh(prm, pb, r0, tile_rows, tile_keys, 0);
+  const Share sh(prm, pb, r0, tile_rows, tile_keys, 0, r.splits);
   if (sh.active == 1) return;
   const int rows = min(tile_rows, pb.R - r0), mine = min(per, rows - ch * per);
-  join_splits<D, BF16, false>(prm, pb, sh.active, (static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits * tile_rows, tile_rows, r0, ch * per, mine,
-                              prm.splits < kJoinApart ? rows : mine, other, threadIdx.x);
+  join_splits<D, BF16, false>(prm, pb, sh.active, static_cast<size_t>(r.slot + (level * r.count + i) * r.splits) * tile_rows, tile_rows, r0, ch * per, mine,
+                              prm.most_splits < kJoinApart ? rows : mine, other, threadIdx.x);
 }
 
-hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * p.splits), block(64 * kRowsWaves);
+hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, int workgroups, hipStream_t s) {
+  const dim3 grid(workgroups), block(64 * kRowsWaves);
   if (head_dim == 128 && eight) {
     hipLaunchKernelGGL((attend_rows<128, true>), grid, block, 0, s, p);
   } else if (head_dim == 128) {
@@ -230,18 +235,19 @@ hipError_t launch_attend_rows(int head_dim, bool eight, const AttendParams& p, h
   return hipGetLastError();
 }
 
-hipError_t launch_attend_join(int head_dim, bool bf16, int tile_rows, int tile_keys, int rows_max, const AttendParams& p, hipStream_t s) {
-  const int per = p.splits >= kJoinApart && static_cast<int64_t>(p.n) * rows_max <= 2048 ? 1 : 8;
+hipError_t launch_attend_join(int head_dim, bool bf16, int tile_rows, int tile_keys, int rows_max, int problems, int tiles, AttendParams& p, hipStream_t s) {
+  const int per = p.most_splits >= kJoinApart && static_cast<int64_t>(problems) * rows_max <= 2048 ? 1 : 8;
   const int chunks = (std::min(rows_max, tile_rows) + per - 1) / per;  // of a tile of rows
-  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * chunks), block(kJoinThreads);
+  for (int i = 0; i < p.runs; ++i) p.start[i] *= chunks;
+  const dim3 grid(tiles * chunks), block(kJoinThreads);
   if (head_dim == 128 && bf16) {
-    hipLaunchKernelGGL((attend_join<128, true>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
+    hipLaunchKernelGGL((attend_join<128, true>), grid, block, 0, s, tile_rows, tile_keys, per, chunks, p);
   } else if (head_dim == 128) {
-    hipLaunchKernelGGL((attend_join<128, false>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
+    hipLaunchKernelGGL((attend_join<128, false>), grid, block, 0, s, tile_rows, tile_keys, per, chunks, p);
   } else if (bf16) {
-    hipLaunchKernelGGL((attend_join<64, true>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
+    hipLaunchKernelGGL((attend_join<64, true>), grid, block, 0, s, tile_rows, tile_keys, per, chunks, p);
   } else {
-    hipLaunchKernelGGL((attend_join<64, false>), grid, block, 0, s, p, tile_rows, tile_keys, per, chunks);
+    hipLaunchKernelGGL((attend_join<64, false>), grid, block, 0, s, tile_rows, tile_keys, per, chunks, p);
   }
   return hipGetLastError();
 }

@@ -148,10 +148,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, D == 128 ? 2 : 3) void attend_rows
   __shared__ __align__(16) char lds[kRowsWaves * kRowsKeys * D * 2];
   __shared__ float ml[2][kRowsWaves][kRows16];
   static_assert(sizeof(lds) >= kRowsWaves * 3 * kQuarter * 64 * 4 && sizeof(lds) >= kJoinThreads * 24, "O^T, join_splits");
-  const int p = blockIdx.x % prm.n, split = blockIdx.x / prm.n;  // (one tile of rows a problem)
-  const Seen pb(prm, p);
+  const AttendPiece piece = piece_of(prm, prm.base + blockIdx.x);  // (one tile of rows a problem)
+  const int split = piece.split;
+  const Seen pb(prm, piece.p);
   if (!pb.has(prm, 0)) return;
-  const Share sh(prm, pb, 0, kRows16, kRowsKeys, split);
+  const Share sh(prm, pb, 0, kRows16, kRowsKeys, split, piece.splits);
   if (split >= sh.active) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), part = lane >> 4;
   const int row = lane & 15, rr = min(row, pb.R - 1), tok = rr / pb.group, head = rr % pb.group;
@@ -236,20 +237,20 @@ __global__ __launch_bounds__(64 * kRowsWaves, D == 128 ? 2 : 3) void attend_rows
     if (pb.d.lse && wave == 0 && part == 0)
       as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(top + fast_log2(total)) : -kInf;
   } else {
-    const size_t at = (static_cast<size_t>(p) * prm.splits + split) * kRows16 + row;
+    const size_t at = static_cast<size_t>(piece.slot + split) * kRows16 + row;
     if (there) {
 #pragma unroll
       for (int x = 0; x < kQuarter; x += 4)
         to_others(prm.part + at * D + 16 * ((wave * kQuarter + x) >> 2) + 4 * part, f32x4{own[x], own[x + 1], own[x + 2], own[x + 3]});
       if (wave == 0 && part == 0) to_others(prm.part_ml + at, f32x2{top, total});
     }
-    if (prm.meet && last_to_come(prm.meet + p, sh.active, tid))
+    if (prm.meet && last_to_come(prm.meet + piece.slot, sh.active, tid))
       join_splits<D, true, true>(prm, pb, sh.active, at - row - static_cast<size_t>(split) * kRows16, kRows16, 0, 0, pb.R, pb.R, ex, tid);
   }
 }
 
-hipError_t launch_attend_rows16(int head_dim, bool eight, const AttendParams& p, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(p.n) * p.splits), block(64 * kRowsWaves);
+hipError_t launch_attend_rows16(int head_dim, bool eight, const AttendParams& p, int workgroups, hipStream_t s) {
+  const dim3 grid(workgroups), block(64 * kRowsWaves);
   if (head_dim == 128 && eight) {
     hipLaunchKernelGGL((attend_rows16<128, true>), grid, block, 0, s, p);
   } else if (head_dim == 128) {

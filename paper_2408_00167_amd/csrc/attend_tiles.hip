@@ -70,11 +70,12 @@ template <int D, bool EIGHT>
 __global__ __launch_bounds__(kThreads, 2) void attend_tiles(AttendParams prm) {
   constexpr int kBuf = kTilesKeys * D * 2;
   extern __shared__ __align__(16) char lds[];  // two tiles of K, two of V
-  const int p = blockIdx.x % prm.n, rest = blockIdx.x / prm.n, rt = prm.row_tiles - 1 - rest % prm.row_tiles, split = rest / prm.row_tiles;
-  const Seen pb(prm, p);
-  const int r0 = rt * kTilesRows;
+  const AttendPiece piece = piece_of(prm, prm.base + blockIdx.x);
+  const int split = piece.split;
+  const Seen pb(prm, piece.p);
+  const int r0 = piece.rt * kTilesRows;
   if (!pb.has(prm, r0)) return;
-  const Share sh(prm, pb, r0, kTilesRows, kTilesKeys, split);
+  const Share sh(prm, pb, r0, kTilesRows, kTilesKeys, split, piece.splits);
   if (split >= sh.active) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), h = lane >> 5;
   const int w0 = r0 + wave * 32, row = lane & 31, rr = min(w0 + row, pb.R - 1), tok = rr / pb.group, head = rr % pb.group;
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(AttendParams prm) {
     if (pb.d.lse && h == 0)
       as_global_mut<float>(pb.d.lse)[head * pb.d.n_que + tok] = total > 0.f ? from_log2(st.ref + fast_log2(total)) : -kInf;
   } else {
-    const size_t at = ((static_cast<size_t>(p) * prm.row_tiles + rt) * prm.splits + split) * kTilesRows + wave * 32 + row;
+    const size_t at = static_cast<size_t>(piece.slot + split) * kTilesRows + wave * 32 + row;
     float* to = prm.part + at * D;
 #pragma unroll
     for (int v = 0; v < D / 2; v += 4) {
@@ -235,8 +236,8 @@ hipError_t set_max_lds_attend() {
   return e;
 }
 
-hipError_t launch_attend_tiles(int head_dim, bool eight, const AttendParams& p, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(p.n) * p.row_tiles * p.splits), block(kThreads);
+hipError_t launch_attend_tiles(int head_dim, bool eight, const AttendParams& p, int workgroups, hipStream_t s) {
+  const dim3 grid(workgroups), block(kThreads);
   const size_t lds = 2 * 2 * static_cast<size_t>(kTilesKeys) * head_dim * 2;
   if (head_dim == 128 && eight) {
     hipLaunchKernelGGL((attend_tiles<128, true>), grid, block, lds, s, p);

@@ -1,4 +1,6 @@
 """finch_attend in the ways it is called: eagerly and in a replayed graph, many problems of different length in one batch."""
+import random
+
 import pytest
 import torch
 
@@ -52,4 +54,57 @@ def test_a_replayed_call_has_the_eager_call_s_bits(dtype, d, G, block, shapes):
             assert torch.equal(pb["full"], out) and torch.equal(pb["lse_full"], lse), f"{dtype} d={d} G={G} {s} replay {replay}"
         fin.attend(batch)
         torch.cuda.synchronize()
+    fin.close()
+
+
+def unlike(rng, n_long, heads):
+    """Requests of all kinds, each with a few problems: more groups of like problems than a launch's table has room for."""
+    shapes = []
+    for i in range(80):
+        n = rng.choice([0, 1, 1, 2, 4, 9, 20, rng.randint(1, 90)])
+        shapes += [(n, rng.choice([0, 1, 40, rng.randint(0, 600)]), n + rng.choice([0, 0, 3]))] * rng.choice([1, heads])
+    for at in (0, 30, 70):
+        shapes.insert(at, (n_long, 9000 + at, n_long))
+    return shapes
+
+
+@pytest.mark.parametrize("dtype,d,G,block", [("bf16", 128, 4, 0), ("bf16", 64, 1, 0), ("bf16", 128, 4, 32), ("f32", 64, 2, 0)])
+@pytest.mark.parametrize("n_long", [1, 12, 70])
+def test_unlike_problems_in_one_batch(dtype, d, G, block, n_long):
+    rng = random.Random(n_long)
+    fin, gen = F.Finch(F.FINCH_BF16 if dtype == "bf16" else F.FINCH_F32, d, G), torch.Generator().manual_seed(22)
+    fin.set_scale_block(block or 64)
+    shapes = unlike(rng, n_long, 2)
+    pbs = [problem(gen, dtype, d, G, *s, causal=i % 5 != 0, eight=block, lse=i % 3 != 0) for i, s in enumerate(shapes)]
+    batch = F.AttentionBatch(pbs)
+    fin.attend(batch)
+    torch.cuda.synchronize()
+    for s, pb in zip(shapes, pbs):
+        verify(pb, f"{dtype} d={d} G={G} block={block} {s}", block or 64)
+    eager = [pb["full"].clone() for pb in pbs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        fin.attend(batch)
+    for _ in range(3):
+        for pb in pbs:
+            pb["out"].fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        for s, pb, out in zip(shapes, pbs, eager):
+            assert torch.equal(pb["full"], out), s
+    fin.close()
+
+
+def test_more_tiles_of_rows_than_a_launch_has_workgroups():
+    """Five problems of 2^24 rows (2^20 tiles each): two launches.  One query row for all, one key: every output is its value."""
+    fin, gen, n = F.Finch(F.FINCH_F32, 64, 1), torch.Generator().manual_seed(23), 1 << 24
+    pbs = []
+    for i in range(5):
+        q, k, v = (torch.randn(1, 64, generator=gen).cuda() for _ in range(3))
+        pbs.append(dict(q=q[:, None].expand(n, 1, 64), k_cache=k, v_cache=v, out=torch.full((n, 1, 64), 7.0, device="cuda"), causal=False))
+    fin.attend(F.AttentionBatch(pbs))
+    torch.cuda.synchronize()
+    for i, pb in enumerate(pbs):
+        for part in pb["out"].view(16, -1, 64):
+            assert bool((part == pb["v_cache"]).all()), i
     fin.close()
