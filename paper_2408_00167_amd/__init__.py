@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import weakref
 from typing import Dict, List, Optional, Sequence
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -195,8 +196,8 @@ def _check(status: int, where: str, ctx=None):
 
 # ------------------------------------------------------------------ C ABI mirrors
 
-# FINCH_OPT_SCALE_BLOCK of the contexts where it was set: how many scales a call reads or writes goes by it
-_scale_blocks: Dict[int, int] = {}
+# The Finch of each context handle: it has to know FINCH_OPT_SCALE_BLOCK however that is set, as its checks of scales go by it.
+_finches = weakref.WeakValueDictionary()
 
 
 def finch_create(dtype: int, head_dim: int, group_size: int) -> ctypes.c_void_p:
@@ -204,12 +205,11 @@ def finch_create(dtype: int, head_dim: int, group_size: int) -> ctypes.c_void_p:
     cfg = finch_config(dtype, head_dim, group_size, 0)
     ctx = ctypes.c_void_p()
     _check(lib.finch_create(ctypes.byref(cfg), ctypes.byref(ctx)), "finch_create")
-    _scale_blocks.pop(ctx.value, None)
     return ctx
 
 
 def finch_destroy(ctx) -> None:
-    _scale_blocks.pop(getattr(ctx, "value", ctx), None)
+    _finches.pop(getattr(ctx, "value", ctx), None)
     _check(load_library().finch_destroy(ctx), "finch_destroy")
 
 
@@ -283,7 +283,9 @@ def finch_profile_read(ctx) -> Dict[str, Dict[str, float]]:
 def finch_set_option(ctx, option: int, value: int) -> None:
     _check(load_library().finch_set_option(ctx, option, value), "finch_set_option", ctx)
     if option == FINCH_OPT_SCALE_BLOCK:
-        _scale_blocks[getattr(ctx, "value", ctx)] = value
+        fin = _finches.get(getattr(ctx, "value", ctx))
+        if fin is not None:
+            fin.scale_block, fin.key = value, tuple(list(fin.key))  # (another key: batches are looked over again)
 
 
 def finch_set_reposition(ctx, pairing: int = FINCH_ROPE_OFF, order: int = FINCH_ORDER_ASCENDING,
@@ -481,6 +483,7 @@ class RowsBatch:
         self.n = len(requests)
         self.host = (finch_rows * max(1, self.n))()
         self.key = self.suits = self.index = None  # (dtype, channels, query heads per KV head or None); the context's it suits; its GPU
+        self.min_block, self.block = 1, None  # (no scales)
         for i, r in enumerate(requests):
             d = self.host[i]
             _on_one_gpu(self, [r.get(name) for name in ("q", "k", "v", "q_out", "k_out", "v_out", "pos", "slot")])
@@ -646,19 +649,15 @@ class Finch:
         self.device = torch.device(self.device.type, self.index)  # (the workspace's as well, whatever device is current later)
         with torch.cuda.device(self.index):  # (a context is bound to the device that is current when it is made)
             self.ctx = finch_create(dtype, head_dim, group_size)
-        self.handle = self.ctx.value
+        _finches[self.ctx.value] = self
         self.ws = None
         self.key = (torch.bfloat16 if dtype == FINCH_BF16 else torch.float32, head_dim, group_size)
-
-    @property
-    def scale_block(self) -> int:
-        """Rows that share a power of two in 8-bit caches, whichever way the context's option was set."""
-        return _scale_blocks.get(self.handle, 64)
+        self.scale_block = 64  # rows that share a power of two in 8-bit caches (set_scale_block)
 
     def close(self):
         if self.ctx is not None:
             finch_destroy(self.ctx)
-            self.ctx = self.handle = None
+            self.ctx = None
 
     def __del__(self):
         try:
@@ -755,14 +754,12 @@ class Finch:
             raise ValueError(f"{what}: batch of {key}, context of {self.key}")
         if batch.index not in (None, self.index):
             raise ValueError(f"{what}: batch on GPU {batch.index}, context on {self.index}")
-        batch.suits = self.key
-
-    def _scales(self, batch, block: int, what: str) -> None:
-        """Scales are read and written by the context's block of rows: there have to be enough, and for that block."""
-        if batch.min_block > block:
+        # scales are read and written by the context's block of rows: there have to be enough, and for that block
+        if batch.min_block > self.scale_block:
             raise ValueError(f"{what}: too few scales for blocks of this size")
-        if batch.block not in (None, block):
-            raise ValueError(f"{what}: scales for blocks of {batch.block} rows, context set to {block}")
+        if batch.block not in (None, self.scale_block):
+            raise ValueError(f"{what}: scales for blocks of {batch.block} rows, context set to {self.scale_block}")
+        batch.suits = self.key
 
     def _stream(self, stream):
         """The stream's handle; the current one's without the 3 us that an object for it takes."""
@@ -785,9 +782,6 @@ class Finch:
         """Rows of K and V as e4m3 with one power of two per block of rows."""
         if batch.suits is not self.key:
             self._suits(batch, "quantize")
-        block = _scale_blocks.get(self.handle, 64)
-        if batch.min_block > block or batch.block is not None:
-            self._scales(batch, block, "quantize")
         st = self.lib.finch_quantize(self.ctx, batch.host, batch.dev_ptr, batch.n, self._stream(stream))
         if st:
             _check(st, "finch_quantize", self.ctx)
@@ -802,9 +796,6 @@ class Finch:
         """Attention over [cache ; chunk]."""
         if batch.suits is not self.key:
             self._suits(batch, "attend")
-        block = _scale_blocks.get(self.handle, 64)
-        if batch.min_block > block or batch.block is not None:
-            self._scales(batch, block, "attend")
         if batch.planned is None or batch.planned[0] is not self or self.ws is None or self.ws.numel() < batch.planned[1]:
             self.reserve_attend(batch)
         st = self.lib.finch_attend(self.ctx, batch.host, batch.dev_ptr, batch.n, self.ws.data_ptr(), self.ws.numel(), self._stream(stream))
