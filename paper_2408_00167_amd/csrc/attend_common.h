@@ -57,7 +57,8 @@ __host__ __device__ __forceinline__ AttendRun run_of(const AttendParams& prm, in
   AttendRun r = prm.one;
 #ifdef __HIP_DEVICE_COMPILE__
   // (now and together: left to itself the compiler fetches each where it is used, one round trip after the other)
-  asm volatile("" : "+s"(r.problem), "+s"(r.count), "+s"(r.top), "+s"(r.levels), "+s"(r.splits), "+s"(r.slot) : "s"(prm.descs), "s"(prm.runs));
+  asm("" : "+s"(r.problem), "+s"(r.count), "+s"(r.top), "+s"(r.levels), "+s"(r.splits), "+s"(r.slot)
+      : "s"(prm.descs), "s"(prm.runs), "s"(prm.group), "s"(prm.rows_lo), "s"(prm.rows_hi), "s"(prm.span));
 #endif
   if (prm.runs > 1) {
     int e = 0;

@@ -98,6 +98,17 @@ def test_alike_problems_are_one_run_in_the_batch_s_order():
     assert got["splits"] == 12 and [x[:3] for x in got["pieces"]] == [(p, 0, s) for s in range(12) for p in range(8)]
 
 
+def test_one_run_where_all_workgroups_are_on_the_chip_at_once():
+    """Nothing is looked up then: problems come in the batch's order, with the most splits and tiles of rows of any."""
+    got = check([(1, c, 1, 1) for c in (4331, 4464, 7414, 3751) for _ in range(5)], G=3)[FEW]
+    assert got["splits"] == 24 and [x[:3] for x in got["pieces"]] == [(p, 0, s) for s in range(24) for p in range(20)]
+    got = check([(n, 9, n, 1) for n in (387, 348, 264) for _ in range(8)], d=64)[MANY]
+    assert [x[:2] for x in got["pieces"]] == [(p, rt) for rt in reversed(range(7)) for p in range(24)]
+    # nor where none of them has nothing to do
+    got = check([(1, c, 1, 1) for c in (6, 40, 6, 60) * 200], G=1)[FEW]
+    assert [x[0] for x in got["pieces"]] == list(range(800))
+
+
 @pytest.mark.parametrize("others", [8, 64, 128, 512, 1016])
 @pytest.mark.parametrize("first", [True, False])
 def test_many_rows_on_a_long_cache_keep_their_splits_beside_tokens(others, first):
