@@ -389,7 +389,8 @@ finch_status finch_rope_frequencies(int32_t dims, double base, const finch_rope_
  * and e >= -100 (e = 0 for a block of zeros), held as the byte e + 127, and its rows hold the
  * e4m3 numbers nearest to x / 2^e (ties to even): a value loses at most 2^-4 of itself, or
  * 2^(e-10) where it is below 2^(e-6).  No value overflows, and the products by powers of
- * two are exact, so the bytes do not depend on how they are computed. */
+ * two are exact, so the bytes do not depend on how they are computed.  The rows may be fp32;
+ * the caches are read by bf16 contexts (finch_attend). */
 typedef struct {
   const void* k;    /* [n] rows in the context's dtype, in_row elements apart */
   const void* v;
@@ -414,8 +415,8 @@ finch_status finch_quantize(finch_ctx* ctx, const finch_quantization* host_desc,
  * With k_scale and v_scale (both or neither, bf16 contexts only) the cache rows are those of
  * finch_quantize, and cache_row counts bytes.  With m_live the chunk has min(m, max(0,
  * *m_live)) rows when the kernel runs, so that a captured step can go on being replayed
- * while its chunk grows.  q and out may be views of [token][head][channel] arrays of a packed
- * batch.  `out` must overlap neither q nor candidates, nor lie over itself: one of its two strides
+ * while its chunk grows.  A replayed call has the bits of the eager one.  q and out may be views of [token][head][channel] arrays of a packed
+ * batch.  `out` must overlap neither q nor candidates (nor lie between their rows), nor lie over itself: one of its two strides
  * must step over all of the other's. */
 typedef struct {
   const void* q;          /* row i of head g: q + i*q_row + g*q_head                    */

@@ -637,7 +637,10 @@ class AttentionBatch:
 
 class Finch:
     """A context plus a workspace tensor that grows on demand (outside any timed
-    or captured region the caller should pre-size it with `reserve`)."""
+    or captured region the caller should pre-size it with `reserve`, `reserve_loop` or
+    `reserve_attend`).  A captured call goes on using the workspace of its time: keep a
+    reference to `ws` beside the graph, as a later call that needs more replaces it.  Batches and the
+    tensors in them are the caller's to keep until the work on them is done."""
 
     def __init__(self, dtype: int, head_dim: int, group_size: int, device="cuda"):
         import torch

@@ -5,7 +5,7 @@
 // A workgroup takes a few tokens of one request with all their heads: sine and cosine of a token's
 // pairs are computed once (angles reduced in fp64) and shared through LDS.  A thread takes two 16-byte
 // pieces of a head, chosen so that it holds both sides of its pairs in either pairing, in turn one
-// of the queries', the keys' and the values' heads; the norm's sum goes over the 8 or 16 lanes
+// of the queries', the keys' and the values' heads; the norm's sum goes over the 4, 8 or 16 lanes
 // that hold a head.
 #include "attend.h"
 #include "reposition_common.h"
