@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2408_00167_amd as F
+from tests.test_attend_plan_cpu import plan
 from tests.test_gpu_attend import problem, verify
 
 pytestmark = pytest.mark.gpu
@@ -107,4 +108,25 @@ def test_more_tiles_of_rows_than_a_launch_has_workgroups():
     for i, pb in enumerate(pbs):
         for part in pb["out"].view(16, -1, 64):
             assert bool((part == pb["v_cache"]).all()), i
+    fin.close()
+
+
+@pytest.mark.parametrize("dtype,d,G,n,kernel", [("bf16", 64, 4, 1, 0), ("bf16", 64, 4, 6, 1), ("f32", 64, 2, 1, 1)])
+def test_ragged_requests_whose_last_splits_join(dtype, d, G, n, kernel):
+    """Many runs, of one to a few splits each: the last split of each tile of rows joins the others."""
+    rng = random.Random(5)
+    lengths = [rng.randint(30, 2500) for _ in range(30)]
+    shapes = [(n, c, n + 2) for c in lengths for _ in range(24)]
+    how = plan([(*s, 1) for s in shapes], kernel, G, d, F.FINCH_BF16 if dtype == "bf16" else F.FINCH_F32)
+    assert 1 < how["splits"] < 16 and how["workgroups"] > 512 and len({x[3] for x in how["pieces"]}) > 1
+    fin, gen = F.Finch(F.FINCH_BF16 if dtype == "bf16" else F.FINCH_F32, d, G), torch.Generator().manual_seed(24)
+    pbs = [problem(gen, dtype, d, G, *s) for s in shapes]
+    batch = F.AttentionBatch(pbs)
+    for again in range(2):  # (the counters are back at zero)
+        for pb in pbs:
+            pb["out"].fill_(9)
+        fin.attend(batch)
+        torch.cuda.synchronize()
+        for i in range(again, len(pbs), 3):
+            verify(pbs[i], f"{dtype} {shapes[i]}")
     fin.close()
