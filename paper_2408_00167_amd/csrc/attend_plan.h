@@ -15,6 +15,7 @@ namespace finch {
 // 128 rows on 20000 keys 45 and 32.
 constexpr int kSomeRows = 64;
 constexpr int kLaunchGrid = (1 << 22) - 1;  // workgroups of a launch: fewer than 2^32 threads
+constexpr int64_t kMostPieces = int64_t{1} << 30;  // workgroups of a batch: their numbers are 32 bits
 
 // Neighbours in a batch with as many tiles of rows and of keys; where a batch has more such groups than a launch has runs,
 // neighbours that are near to it, with the most of either (and what lies between them).
@@ -113,6 +114,7 @@ struct AttendLaunch {
 
   finch_status deal(bool many, int64_t cu, int head_dim, int heads, size_t& off) {
     if (tiles == 0) return FINCH_OK;
+    if (tiles > kMostPieces) return FINCH_ERR_CAPACITY;
     choose_span(many, cu);
     // partial results of at most 64 MiB, and a counter for each
     const int64_t bytes = int64_t{tile_rows} * (head_dim + 2) * 4, most = std::min<int64_t>((int64_t{64} << 20) / bytes, kAttendMeetWords);
@@ -165,7 +167,7 @@ struct AttendLaunch {
       start[r] = workgroups;
       workgroups += int64_t{run[r].count} * run[r].levels * run[r].splits;
     }
-    if (workgroups > (int64_t{1} << 30)) return FINCH_ERR_CAPACITY;
+    if (workgroups > kMostPieces) return FINCH_ERR_CAPACITY;
     if (slots > 0) {
       off_o = off = std::max<size_t>(off, 256);  // (behind the status word that other calls keep there)
       off = align_up(off + static_cast<size_t>(slots) * tile_rows * head_dim * 4, 256);
